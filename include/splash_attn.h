@@ -366,6 +366,185 @@ int splash_mla_plan_host(const int32_t* seq_lens_host, int32_t q_chunk,
                          int32_t max_partials, int32_t* units_out, int32_t max_units,
                          int32_t* indptr_out, int32_t* stats_out, int32_t* worker_start_out);
 
+/*
+ * ---- the serving step around grouped-query attention -----------------------
+ *
+ * For models with a few KV heads instead of one shared latent row: num_heads
+ * query heads share num_kv_heads K and V heads (query head h reads KV head
+ * h / (num_heads / num_kv_heads)), and K and V are kept in 8 bits.  One step:
+ *   splash_step_tables   the new tokens' pages, slots and positions
+ *   splash_rope          rotary positions on the step's queries and keys
+ *   splash_gqa_append    the new K and V rows into the cache
+ *   splash_gqa_attend    attention of the step's query rows
+ * splash_step_tables and splash_rope serve the MLA calls above as well: the
+ * block table and slots are the same, and the rotary part of a packed query
+ * row or a latent row is a strided view.
+ *
+ * These four calls stay inside their buffers whatever the device data holds:
+ * lengths are clamped to the block-table row, a block-table entry or slot
+ * outside the pool is skipped (that is how a page that splash_step_tables
+ * could not get is passed on), and a row that sees no key gets out = 0 and
+ * lse = -inf.  All of them can be captured in a graph.
+ *
+ * Cache: a block is the 64 tokens of one page for one KV head,
+ *   k_pages, v_pages    [num_pages, num_kv_heads, 64, head_dim] codes, one byte each
+ *   k_scales, v_scales  fp32 [num_pages, num_kv_heads], finite and > 0:
+ *                       value = code * scale of its block
+ * A block's scale as splash_gqa_append writes it is a power of two, so that a
+ * growing block is brought to a new scale by shifting its codes' exponents.
+ */
+#define SPLASH_GQA_E4M3 0   /* codes: OCP E4M3 ("fn") bytes */
+#define SPLASH_GQA_INT8 1   /* codes: signed bytes */
+
+typedef struct splash_gqa_desc {
+    int32_t batch;              /* B: requests (0: every call is a no-op) */
+    int32_t num_heads;          /* query heads, a multiple of num_kv_heads, at most 1024 */
+    int32_t num_kv_heads;       /* 1 .. 128 */
+    int32_t head_dim;           /* 64, 128 or 256 */
+    int32_t page_size;          /* must be 64 */
+    int32_t max_pages_per_seq;  /* row stride of block_table, at least 1 */
+    int32_t num_pages;          /* pages in the pool, 1 .. 2^25 */
+    int32_t code_type;          /* SPLASH_GQA_* */
+    float softmax_scale;        /* multiplies <q, k>; finite and > 0 */
+} splash_gqa_desc;
+
+/*
+ * splash_step_tables: block table, slots and positions of a step's new tokens
+ * from the requests' lengths.  Request b's history has s_b = seq_lens[b]
+ * tokens after the step, the last n_b of them new (n_b = new_lens[b], or
+ * q_chunk where new_lens is NULL); 0 <= s_b <= 64 * max_pages_per_seq and
+ * 0 <= n_b <= s_b (values outside are clamped).  Pages ceil((s_b - n_b) / 64)
+ * .. ceil(s_b / 64) - 1 of the request are new and are taken from the free
+ * list in the order of the requests:
+ *   free_pages   int32 [num_free] pages that no request holds
+ *   taken_in     int32 [2]; [0] entries of the list taken by earlier steps
+ *                (clamped to [0, num_free]), [1] is not read
+ *   taken_out    int32 [2]; [0] entries taken after this step, [1] new pages
+ *                that the list had no entry for (0: every page was found).
+ *                Must not overlap taken_in; the next step's taken_in.
+ *   block_table  int32 [B, max_pages_per_seq]; the new pages' entries are
+ *                written (-1 where the list has run out), all others are left
+ *                as they are
+ *   new_indptr   int32 [B+1]: request b's new tokens are rows
+ *                new_indptr[b] .. new_indptr[b+1] - 1 of the step
+ *   slots        int32 [max_tokens]: 64 * page + place in the page of every
+ *                row's token, -1 where its block-table entry is outside
+ *                [0, num_pages) and on the rows behind the last new token
+ *   positions    int32 [max_tokens]: the token's place in its history (0 on
+ *                the rows behind)
+ *   requests     int32 [max_tokens]: the row's request (-1 on the rows behind)
+ * Rows past max_tokens are not written; new_indptr counts them.  One launch.
+ * Errors: INVALID_ARGUMENT (NULL buffer, batch or max_tokens or num_free < 0,
+ * q_chunk < 0, max_pages_per_seq < 1, num_pages < 1, taken_out == taken_in),
+ * MISALIGNED (a buffer not 4-byte aligned), UNSUPPORTED (batch > 8192,
+ * num_pages > 2^25, 64 * max_pages_per_seq * batch past 2^31 - 1).
+ */
+int splash_step_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t q_chunk, int32_t batch,
+                       const int32_t* free_pages, int32_t num_free, const int32_t* taken_in, int32_t* taken_out,
+                       int32_t* block_table, int32_t max_pages_per_seq, int32_t num_pages, int32_t max_tokens,
+                       int32_t* new_indptr, int32_t* slots, int32_t* positions, int32_t* requests, void* stream);
+
+/*
+ * splash_rope: rotary positions with one to four axes (text: one; video and
+ * images: time, height, width).  Pair j of a row (j < rot_dim / 2) turns by
+ *   angle = positions[axis_j][n] * inv_freq[j]
+ *   (a, b) -> scale * (a cos - b sin, b cos + a sin)
+ * with (a, b) = (x[j], x[j + rot_dim / 2]), or (x[2j], x[2j + 1]) where
+ * `interleaved`.  The angle is formed and reduced to a turn's fraction in 64
+ * bits (so far positions lose nothing), sine, cosine and products are fp32,
+ * rounded once to bf16.  Up to two tensors (a step's queries and keys) turn in one launch.
+ *   view   x, y: bf16, element d of head h of token n at
+ *          n * token_stride + h * head_stride + d (strides in elements, of x
+ *          and y each); y == x with the same strides rotates in place, else
+ *          the two must not overlap.  Only rot_dim elements of a head are read
+ *          and written.
+ *   positions  int32, axis a's position of token n at [a * position_stride + n];
+ *          position_stride >= num_tokens where num_axes > 1
+ * inv_freq and pair_axis are HOST arrays of rot_dim / 2, read during the call.
+ * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, num_axes outside
+ * 1 .. 4, an axis outside [0, num_axes), an inv_freq or scale that is not
+ * finite), UNSUPPORTED (rot_dim odd or outside 2 .. 256, more than 65536
+ * heads), MISALIGNED (x or y not 2-byte, positions not 4-byte aligned).
+ */
+typedef struct splash_rope_view {
+    const void* x;
+    void* y;
+    int64_t x_token_stride, x_head_stride;
+    int64_t y_token_stride, y_head_stride;
+    int32_t num_heads;
+} splash_rope_view;
+
+typedef struct splash_rope_desc {
+    int32_t rot_dim;            /* even, 2 .. 256 */
+    int32_t interleaved;        /* 0: pairs (j, j + rot_dim / 2); 1: pairs (2j, 2j + 1) */
+    int32_t num_axes;           /* 1 .. 4 */
+    float scale;                /* multiplies the turned pair (1: none) */
+    const double* inv_freq;     /* host [rot_dim / 2], radians per position */
+    const uint8_t* pair_axis;   /* host [rot_dim / 2], the axis of each pair; NULL: axis 0 */
+} splash_rope_desc;
+
+int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t* positions, int64_t position_stride,
+                int32_t num_tokens, const splash_rope_desc* desc, void* stream);
+
+/*
+ * splash_gqa_append: new K and V rows into their blocks.
+ *   k_new, v_new  bf16, element d of KV head h of row t at
+ *                 t * token_stride + h * head_stride + d (elements, one pair of
+ *                 strides for both: views of a fused projection's rows)
+ *   slots         int32 [num_tokens]; row t goes to place slots[t] % 64 of page
+ *                 slots[t] / 64; a slot outside [0, 64 * num_pages) is skipped.
+ *                 Slots are distinct, and the rows of one page stand next to
+ *                 each other in the list (as splash_step_tables writes them).
+ * With TOP = 448 (E4M3) or 127 (INT8), for every block that gets rows:
+ *   e   = the least e >= -126 with |x| <= TOP * 2^e for every finite new x;
+ *         not below the block's own exponent, unless a new row takes place 0,
+ *         which starts the block anew
+ *   rows before the last new place that are not new: code -> code * old scale
+ *         * 2^-e, rounded to nearest even (only where the scale grows)
+ *   new rows: code = x * 2^-e, rounded to nearest even; infinities take the
+ *         largest code of their sign; NaN is E4M3's NaN and INT8's 0
+ *   scale = 2^e
+ * A block that is continued must have a power-of-two scale (as this call
+ * writes it; of another, its exponent alone is used).  Rows of a block past its
+ * last new place are not written.
+ * Errors: INVALID_ARGUMENT (desc, NULL, num_tokens < 0, negative stride),
+ * UNSUPPORTED (desc), MISALIGNED (pages not 16-byte, scales or slots not 4-byte,
+ * k_new and v_new not 16-byte aligned, strides not multiples of 8 elements).
+ */
+int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride, int64_t head_stride,
+                      const int32_t* slots, int32_t num_tokens, void* k_pages, void* v_pages, float* k_scales,
+                      float* v_scales, const splash_gqa_desc* desc, void* stream);
+
+/*
+ * splash_gqa_attend: attention of q_chunk causal query rows per request.  Row
+ * n = b*q_chunk + i sees keys j = 0 .. s_b - q_chunk + i (none where that is
+ * negative: out = 0, lse = -inf), K_j and V_j from place j % 64 of page
+ * block_table[b*max_pages_per_seq + j/64]:
+ *   z_j        = softmax_scale * <q[n,h,:], K_j>
+ *   lse[n,h]   = ln sum_j exp(z_j)
+ *   out[n,h,:] = sum_j exp(z_j - lse[n,h]) * V_j
+ *   q          bf16 [B*q_chunk, num_heads, head_dim]
+ *   seq_lens   int32 [B], history lengths including the chunk
+ *   out        bf16 [B*q_chunk, num_heads, head_dim] (round to nearest even)
+ *   lse        fp32 [B*q_chunk, num_heads]; may be NULL
+ *   workspace  splash_gqa_workspace_size(desc, q_chunk) bytes, 16-byte aligned
+ * Codes are converted exactly (K to bf16, V to fp16), products are summed in
+ * fp32; a weight is rounded to fp16 before it meets V, and its sum is not.
+ * Codes of places that no row of the request sees are not used, NaN codes
+ * among them, and a place that some rows of a chunk do not see does not touch
+ * those rows.  Deterministic: the same inputs give the same bits, wherever the
+ * pages lie.
+ * Errors: INVALID_ARGUMENT (desc, NULL, q_chunk < 1), UNSUPPORTED (desc;
+ * a batch whose pages times heads pass 2^30), MISALIGNED (q, out, pages or
+ * workspace not 16-byte, other arrays not 4-byte aligned),
+ * WORKSPACE_TOO_SMALL.
+ */
+size_t splash_gqa_workspace_size(const splash_gqa_desc* desc, int32_t q_chunk);
+int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, const float* k_scales,
+                      const float* v_scales, const int32_t* block_table, const int32_t* seq_lens, int32_t q_chunk,
+                      void* out, float* lse, const splash_gqa_desc* desc, void* workspace, size_t ws_bytes,
+                      void* stream);
+
 /* Number of work units the workspace reserves: B*q_chunk + max_partials. */
 int32_t splash_mla_max_units(int32_t batch, int32_t q_chunk, int32_t max_partials);
 

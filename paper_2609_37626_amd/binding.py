@@ -30,6 +30,8 @@ FLAG_DEBUG_CHECK = 1
 FLAG_FORCE_SPLIT = 2
 FLAG_EXACT_QK = 4
 DEFAULT_MAX_PARTIALS = 1024
+GQA_E4M3 = 0
+GQA_INT8 = 1
 
 
 class SplashError(RuntimeError):
@@ -55,6 +57,43 @@ class MlaDesc(ctypes.Structure):
     ]
 
 
+class GqaDesc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("num_heads", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("max_pages_per_seq", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("code_type", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+    ]
+
+
+class RopeView(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("y", ctypes.c_void_p),
+        ("x_token_stride", ctypes.c_int64),
+        ("x_head_stride", ctypes.c_int64),
+        ("y_token_stride", ctypes.c_int64),
+        ("y_head_stride", ctypes.c_int64),
+        ("num_heads", ctypes.c_int32),
+    ]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("inv_freq", ctypes.POINTER(ctypes.c_double)),
+        ("pair_axis", ctypes.POINTER(ctypes.c_uint8)),
+    ]
+
+
 _lib = None
 
 _VP = ctypes.c_void_p
@@ -62,6 +101,8 @@ _I32 = ctypes.c_int32
 _SZ = ctypes.c_size_t
 _PD = ctypes.POINTER(MlaDesc)
 _PI32 = ctypes.POINTER(ctypes.c_int32)
+_I64 = ctypes.c_int64
+_PG = ctypes.POINTER(GqaDesc)
 
 _SIGNATURES = {
     "splash_mla_workspace_size": (_SZ, [_I32, _I32, _I32, _I32]),
@@ -85,6 +126,12 @@ _SIGNATURES = {
     "splash_mla_plan_host": (ctypes.c_int, [_PI32, _I32, _PD, _I32, _I32, _PI32, _I32, _PI32, _PI32, _PI32]),
     "splash_mla_max_units": (_I32, [_I32, _I32, _I32]),
     "splash_device_workers": (_I32, []),
+    "splash_step_tables": (ctypes.c_int, [_VP, _VP, _I32, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _I32, _I32, _VP, _VP, _VP,
+                                          _VP, _VP]),
+    "splash_rope": (ctypes.c_int, [ctypes.POINTER(RopeView), _I32, _VP, _I64, _I32, ctypes.POINTER(RopeDesc), _VP]),
+    "splash_gqa_append": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _I32, _VP, _VP, _VP, _VP, _PG, _VP]),
+    "splash_gqa_workspace_size": (_SZ, [_PG, _I32]),
+    "splash_gqa_attend": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _VP, _VP, _PG, _VP, _SZ, _VP]),
     "splash_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "splash_last_error": (ctypes.c_char_p, []),
     "splash_version": (ctypes.c_char_p, []),
@@ -302,6 +349,179 @@ def splash_mla_plan_host(seq_lens: np.ndarray, q_chunk: int, desc: MlaDesc, num_
     return units[:n].copy(), indptr, {"units": n, "partials": int(stats[1]), "chunk_pages": int(stats[2]),
                                       "total_pages": int(stats[3]), "fold": fold, "cap": int(stats[5]),
                                       "max_parts": int(stats[6]), "worker_start": wstart if fold else None}
+
+
+# ------------------------------ the serving step around grouped-query attention
+#
+# These calls check their tensors against what the kernels assume (type, shape,
+# strides, one device), run on the tensors' device, and take its current stream.
+
+def _refuse(message: str):
+    raise SplashError(SPLASH_ERR_INVALID_ARGUMENT, message)
+
+
+def _device_of(first, **tensors) -> int:
+    """The device of `first`; every tensor is on it, contiguous and of its type."""
+    dev = first.get_device()
+    if dev < 0:
+        _refuse("tensors must be on the GPU")
+    for name, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype not in dtype:
+            _refuse(f"{name} must be {' or '.join(str(d) for d in dtype)} (got {t.dtype})")
+        if shape is not None and tuple(t.shape) != shape:
+            _refuse(f"{name} must have shape {shape} (got {tuple(t.shape)})")
+        if not t.is_contiguous():
+            _refuse(f"{name} must be contiguous")
+        if t.get_device() != dev:
+            _refuse(f"{name} is on another device")
+    return dev
+
+
+def _on_device(dev: int, call, stream) -> None:
+    """call(stream handle) with `dev` current."""
+    import torch
+    if torch._C._cuda_getDevice() == dev:
+        _check(call(_stream(stream)))
+    else:
+        with torch.cuda.device(dev):
+            _check(call(_stream(stream)))
+
+
+def make_gqa_desc(batch: int, num_heads: int, num_kv_heads: int, head_dim: int, max_pages_per_seq: int, num_pages: int,
+                  code_type: int = GQA_E4M3, softmax_scale: Optional[float] = None) -> GqaDesc:
+    """softmax_scale: 1 / sqrt(head_dim) by default."""
+    d = GqaDesc()
+    d.batch = batch
+    d.num_heads = num_heads
+    d.num_kv_heads = num_kv_heads
+    d.head_dim = head_dim
+    d.page_size = 64
+    d.max_pages_per_seq = max_pages_per_seq
+    d.num_pages = num_pages
+    d.code_type = code_type
+    d.softmax_scale = float(np.float32(head_dim ** -0.5 if softmax_scale is None else softmax_scale))
+    return d
+
+
+def gqa_workspace_size(desc: GqaDesc, q_chunk: int) -> int:
+    n = int(lib().splash_gqa_workspace_size(ctypes.byref(desc), q_chunk))
+    if n == 0:
+        _refuse(lib().splash_last_error().decode())
+    return n
+
+
+def make_rope(rot_dim: int, inv_freq, pair_axis=None, num_axes: Optional[int] = None, interleaved: bool = False,
+              scale: float = 1.0) -> RopeDesc:
+    """inv_freq: radians per position of each of the rot_dim / 2 pairs; pair_axis: the position axis of each (0)."""
+    freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+    if freq.shape != (rot_dim // 2,):
+        _refuse(f"inv_freq must hold {rot_dim // 2} frequencies")
+    d = RopeDesc()
+    d.rot_dim = rot_dim
+    d.interleaved = int(bool(interleaved))
+    d.scale = scale
+    d.inv_freq = freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+    d.num_axes = 1
+    d.arrays = [freq]  # (kept alive with the descriptor)
+    if pair_axis is not None:
+        axis = np.asarray(pair_axis, dtype=np.int64)
+        if axis.shape != freq.shape or axis.min() < 0 or axis.max() > 3:
+            _refuse("pair_axis must hold an axis, 0 to 3, for every pair")
+        d.num_axes = int(axis.max()) + 1
+        axis = axis.astype(np.uint8)
+        d.pair_axis = axis.ctypes.data_as(ctypes.POINTER(ctypes.c_uint8))
+        d.arrays.append(axis)
+    if num_axes is not None:
+        d.num_axes = num_axes
+    return d
+
+
+def splash_step_tables(seq_lens, q_chunk: int, free_pages, taken_in, taken_out, block_table, num_pages: int, new_indptr,
+                       slots, positions, requests, new_lens=None, stream=None) -> None:
+    """Pages, slots and positions of the step's new tokens (new_lens[b], or q_chunk of every request)."""
+    import torch
+    i32 = (torch.int32,)
+    b, rows = seq_lens.numel(), slots.numel()
+    dev = _device_of(seq_lens, seq_lens=(seq_lens, i32, (b,)), new_lens=(new_lens, i32, (b,)),
+                     free_pages=(free_pages, i32, None), taken_in=(taken_in, i32, (2,)), taken_out=(taken_out, i32, (2,)),
+                     block_table=(block_table, i32, (b, block_table.shape[-1])), new_indptr=(new_indptr, i32, (b + 1,)),
+                     slots=(slots, i32, (rows,)), positions=(positions, i32, (rows,)), requests=(requests, i32, (rows,)))
+    _on_device(dev, lambda s: lib().splash_step_tables(
+        _ptr(seq_lens), _ptr(new_lens), q_chunk, b, _ptr(free_pages), free_pages.numel(), _ptr(taken_in), _ptr(taken_out),
+        _ptr(block_table), block_table.shape[-1], num_pages, rows, _ptr(new_indptr), _ptr(slots), _ptr(positions),
+        _ptr(requests), s), stream)
+
+
+def _rope_view(view: RopeView, x, y, tokens: int, rot_dim: int, dev: int) -> None:
+    import torch
+    for name, t in (("x", x), ("out", y)):
+        if t.dtype != torch.bfloat16 or t.get_device() != dev:
+            _refuse(f"{name} must be bf16 on the positions' device")
+        if t.dim() != 3 or t.shape[0] != tokens or t.shape[1] != x.shape[1] or t.shape[2] != rot_dim or t.stride(2) != 1:
+            _refuse(f"{name} must be [{tokens}, heads, {rot_dim}] with the last dimension dense (got {tuple(t.shape)}, "
+                    f"strides {t.stride()})")
+    view.x, view.y, view.num_heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+    view.x_token_stride, view.x_head_stride, _ = x.stride()
+    view.y_token_stride, view.y_head_stride, _ = y.stride()
+
+
+def splash_rope(x, positions, rope: RopeDesc, out=None, x2=None, out2=None, stream=None) -> None:
+    """Turns x (and x2) [tokens, heads, rot_dim], views of any token and head stride, by positions [tokens] or
+    [axes, tokens] into out (None: in place)."""
+    import torch
+    pos = positions if positions.dim() == 2 else positions[None]
+    if pos.dim() != 2 or pos.shape[0] != rope.num_axes or pos.dtype != torch.int32 or (pos.shape[1] > 1 and pos.stride(1) != 1):
+        _refuse(f"positions must be int32 [{rope.num_axes}, tokens], dense along the tokens")
+    dev, n = pos.get_device(), pos.shape[1]
+    if dev < 0:
+        _refuse("tensors must be on the GPU")
+    views = (RopeView * 2)()
+    _rope_view(views[0], x, x if out is None else out, n, rope.rot_dim, dev)
+    if x2 is not None:
+        _rope_view(views[1], x2, x2 if out2 is None else out2, n, rope.rot_dim, dev)
+    _on_device(dev, lambda s: lib().splash_rope(views, 1 if x2 is None else 2, _ptr(pos), pos.stride(0), n,
+                                                ctypes.byref(rope), s), stream)
+
+
+def _gqa_cache(desc: GqaDesc, k_pages, v_pages, k_scales, v_scales):
+    import torch
+    codes = (torch.uint8, torch.float8_e4m3fn) if desc.code_type == GQA_E4M3 else (torch.int8,)
+    pool = (desc.num_pages, desc.num_kv_heads, 64, desc.head_dim)
+    f32 = (torch.float32,)
+    return dict(k_pages=(k_pages, codes, pool), v_pages=(v_pages, codes, pool), k_scales=(k_scales, f32, pool[:2]),
+                v_scales=(v_scales, f32, pool[:2]))
+
+
+def splash_gqa_append(k_new, v_new, slots, k_pages, v_pages, k_scales, v_scales, desc: GqaDesc, stream=None) -> None:
+    """Row t of k_new and v_new [rows, kv heads, head_dim] (views of one token and head stride) to slot slots[t]."""
+    import torch
+    n = slots.numel()
+    dev = _device_of(slots, slots=(slots, (torch.int32,), (n,)), **_gqa_cache(desc, k_pages, v_pages, k_scales, v_scales))
+    shape = (n, desc.num_kv_heads, desc.head_dim)
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or t.get_device() != dev:
+            _refuse(f"{name} must be bf16 {shape} on the cache's device")
+    if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
+        _refuse("k_new and v_new must have the same strides, the last dimension dense")
+    _on_device(dev, lambda s: lib().splash_gqa_append(
+        _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(slots), n, _ptr(k_pages), _ptr(v_pages),
+        _ptr(k_scales), _ptr(v_scales), ctypes.byref(desc), s), stream)
+
+
+def splash_gqa_attend(q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, q_chunk: int, out, lse,
+                      desc: GqaDesc, workspace, stream=None) -> None:
+    import torch
+    rows = (desc.batch * q_chunk, desc.num_heads, desc.head_dim)
+    bf16, i32 = (torch.bfloat16,), (torch.int32,)
+    dev = _device_of(q, q=(q, bf16, rows), out=(out, bf16, rows), lse=(lse, (torch.float32,), rows[:2]),
+                     block_table=(block_table, i32, (desc.batch, desc.max_pages_per_seq)),
+                     seq_lens=(seq_lens, i32, (desc.batch,)), workspace=(workspace, (torch.uint8,), None),
+                     **_gqa_cache(desc, k_pages, v_pages, k_scales, v_scales))
+    _on_device(dev, lambda s: lib().splash_gqa_attend(
+        _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(block_table), _ptr(seq_lens), q_chunk,
+        _ptr(out), _ptr(lse), ctypes.byref(desc), _ptr(workspace), workspace.numel(), s), stream)
 
 
 def version() -> str:

@@ -17,16 +17,18 @@
 #include <string>
 #include <vector>
 
+#include "errors.hpp"
 #include "kernels.hpp"
 #include "splash_common.hpp"
 
 using namespace splash;
 
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
 
-int fail(int status, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+namespace splash {
+
 int fail(int status, const char* fmt, ...) {
   char buf[512];
   va_list ap;
@@ -40,6 +42,10 @@ int fail(int status, const char* fmt, ...) {
 int hip_fail(hipError_t e, const char* what) {
   return fail(SPLASH_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace splash
+
+namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

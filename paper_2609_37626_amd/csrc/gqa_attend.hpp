@@ -1,0 +1,423 @@
+// gfx950 kernel of splash_gqa_attend: grouped-query attention over a paged
+// cache of 8-bit codes with one scale per block (64 tokens of one KV head).
+//
+// A tile is one request, one KV head and up to 16*MT of its query rows
+// (q_chunk rows times the heads that share the KV head): every K and V byte is
+// read once for all of them.  A workgroup of four waves takes a tile; wave w
+// takes its pages w, w + 4, ..., one page a step, and the four results are
+// joined through LDS.  Nothing else goes through LDS: each operand is loaded
+// from the cache in the layout that its MFMA reads, because the contraction's
+// order is free as long as both operands agree on it.
+//   QK  S^T[key, row] = K Q^T, v_mfma_f32_16x16x32_bf16.  Lane (g, c), g =
+//       lane / 16, c = lane % 16, holds key c's dims [g D/4, (g+1) D/4) as
+//       contiguous bytes; Q is held the same way.
+//   PV  O^T[dim, row] = V^T P^T, v_mfma_f32_16x16x32_f16.  S^T leaves lane
+//       (g, c) with row c's weights of keys 4g .. 4g+3 of each 16-key group, so
+//       those are the keys it contracts; V^T's lane loads dims [c D/16,
+//       (c+1) D/16) of the same keys, and a byte permutation pairs its keys.
+// The weights 2^(z - m + 6) are taken against a reference m that moves only
+// when a row's maximum passes it by 2^8, so a weight stays below 2^14 and no
+// exchange between lanes is needed on the other steps; 2^6 keeps the small ones
+// off fp16's subnormals.  P is rounded to fp16 (2^-12 relative) for PV.  A
+// block's V scale multiplies its product in fp32, never the weights.
+//
+// Bound: HBM.  A page costs 128 D bytes against 4 D x 64 x 16 MT flops.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "device_types.hpp"
+#include "step.hpp"
+
+namespace splash {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+namespace gqa {
+
+constexpr int kWaves = 4;
+constexpr float kWeightShift = 6.f;   // weights are 2^(z - m + 6)
+constexpr float kMoveAt = 8.f;        // the reference moves once a score passes it by this
+constexpr float kNegInf = -__builtin_inff();
+
+// ---- codes to MFMA operands (exact) --------------------------------------
+
+// Eight codes (two dwords) to bf16.
+template <int CODE>
+__device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t a, uint32_t b) {
+  u32x4 r;
+  if constexpr (CODE == 0) {
+    r[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)a, 1.0f, false));
+    r[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)a, 1.0f, true));
+    r[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, 1.0f, false));
+    r[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)b, 1.0f, true));
+  } else {
+    r[0] = pack_bf16x2((float)(int8_t)a, (float)(int8_t)(a >> 8));
+    r[1] = pack_bf16x2((float)(int8_t)(a >> 16), (float)(int8_t)(a >> 24));
+    r[2] = pack_bf16x2((float)(int8_t)b, (float)(int8_t)(b >> 8));
+    r[3] = pack_bf16x2((float)(int8_t)(b >> 16), (float)(int8_t)(b >> 24));
+  }
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// The codes of one dim (byte `byte` of each dword) of two tokens to fp16.
+// pair holds [t0.b, t1.b, t0.b+1, t1.b+1]; hi selects the second dim.  INT8
+// codes come with their sign bit flipped (code + 128).
+template <int CODE, bool HI>
+__device__ __forceinline__ uint32_t pair_to_f16(uint32_t pair) {
+  if constexpr (CODE == 0) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)pair, 1.0f, HI));
+  } else {
+    // 0x6400 | u is the half 1024 + u, exactly
+    const uint32_t u = __builtin_amdgcn_perm(0x64646464u, pair, HI ? 0x04030402u : 0x04010400u);
+    const f16x2 v = __builtin_bit_cast(f16x2, u) - (f16x2){(_Float16)1152.0f, (_Float16)1152.0f};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+}
+
+__device__ __forceinline__ float xor_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float xor_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// 4-byte pieces as wide as a lane's share of a row.
+template <int N>
+struct Dwords {
+  uint32_t v[N];
+};
+template <int N>
+__device__ __forceinline__ Dwords<N> load_dwords(const uint8_t* p) {
+  Dwords<N> r;
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const u32x4 x = *(const u32x4*)(p + 16 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.v[4 * i + j] = x[j];
+    }
+  } else if constexpr (N == 2) {
+    const u32x2 x = *(const u32x2*)p;
+    r.v[0] = x[0];
+    r.v[1] = x[1];
+  } else {
+    r.v[0] = *(const uint32_t*)p;
+  }
+  return r;
+}
+
+template <int D, int MT>
+struct Shape {
+  static constexpr int kRows = 16 * MT;
+  static constexpr int kSteps = D / 32;     // QK MFMAs per 16 keys and row tile
+  static constexpr int kKDw = D / 16;       // dwords of a lane's share of a K row (D/4 bytes)
+  static constexpr int kVDw = D / 64;       // dwords of a lane's share of a V row (D/16 bytes)
+  static constexpr int kDims = D / 16;      // dims of a lane's share, = MFMA row groups of O^T
+  // the four waves' results are joined kPass dims of each share at a time, in at most 64 KB
+  static constexpr int kPass = (kWaves * kRows * D * 4 <= 65536) ? kDims : 65536 / (kWaves * kRows * 64);
+  static constexpr int kRowStride = 16 * kPass + 4;  // floats, padded by a 16-byte bank group
+};
+
+// One tile's pages [p0, p1) on the four waves.  Writes the normalised rows and
+// their LSE.
+template <int D, int MT, int CODE>
+__device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, int hk, int row0, int seq, int p0, int p1,
+                                             float* lds_o, float* lds_m, float* lds_l) {
+  using S = Shape<D, MT>;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = a.q_chunk * a.group;
+  const int Hq = a.Hk * a.group;
+
+  // queries: row row0 + 16 mt + c, dims [g D/4, ...), eight a step
+  bf16x8 q[MT][S::kSteps];
+  int sees[MT];  // keys that this lane's row sees
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = row0 + 16 * mt + c;
+    const int rr = r < rows ? r : rows - 1;
+    const int i = rr / a.group, h = hk * a.group + rr - i * a.group;
+    const uint16_t* src = a.q + (((int64_t)b * a.q_chunk + i) * Hq + h) * D + g * (D / 4);
+#pragma unroll
+    for (int s = 0; s < S::kSteps; ++s) {
+      u32x4 x = *(const u32x4*)(src + 8 * s);
+      if (r >= rows) x = (u32x4){0, 0, 0, 0};
+      q[mt][s] = __builtin_bit_cast(bf16x8, x);
+    }
+    sees[mt] = seq - a.q_chunk + i + 1;
+  }
+  // keys that every row of the tile sees (a page below it needs no mask), and
+  // that the last row sees
+  const int all_see = seq - a.q_chunk + row0 / a.group + 1;
+
+  f32x4 o[S::kDims][MT];
+  float m[MT], l[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    m[mt] = kNegInf;
+    l[mt] = 0.f;
+#pragma unroll
+    for (int j = 0; j < S::kDims; ++j) o[j][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int32_t* bt = a.block_table + (int64_t)b * a.bt_stride;
+  for (int p = p0 + wave; p < p1; p += kWaves) {
+    const int page = bt[p];
+    if ((unsigned)page >= (unsigned)a.num_pages) continue;
+    const int64_t block = (int64_t)page * a.Hk + hk;
+    const uint8_t* kb = a.k_pages + block * (kPage * D);
+    const uint8_t* vb = a.v_pages + block * (kPage * D);
+    const float ks = a.k_scales[block] * a.scale_log2, vs = a.v_scales[block];
+    const bool masked = 64 * p + 64 > all_see;
+
+    // scores
+    f32x4 z[4][MT];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      const Dwords<S::kKDw> k = load_dwords<S::kKDw>(kb + (16 * kt + c) * D + g * (D / 4));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) z[kt][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < S::kSteps; ++s) {
+        const bf16x8 kf = codes_to_bf16<CODE>(k.v[2 * s], k.v[2 * s + 1]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          z[kt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[mt][s], z[kt][mt], 0, 0, 0);
+      }
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) z[kt][mt] *= ks;
+    }
+    if (masked) {
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (64 * p + 16 * kt + 4 * g + i >= sees[mt]) z[kt][mt][i] = kNegInf;
+    }
+
+    // weights
+    uint32_t w[MT][2][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      float top = kNegInf;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, z[kt][mt][i]);
+      if (__any(top > m[mt] + kMoveAt)) {
+        const float now = fmaxf(m[mt], xor_max(top));
+        const float by = now == kNegInf ? 1.f : __builtin_amdgcn_exp2f(m[mt] - now);
+        m[mt] = now;
+        l[mt] *= by;
+#pragma unroll
+        for (int j = 0; j < S::kDims; ++j) o[j][mt] *= by;
+      }
+      const float ref = m[mt] == kNegInf ? 0.f : m[mt] - kWeightShift;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        float e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          e[i] = __builtin_amdgcn_exp2f(z[kt][mt][i] - ref);
+          l[mt] += e[i];
+        }
+        w[mt][kt >> 1][2 * (kt & 1)] = pack_f16x2(e[0], e[1]);
+        w[mt][kt >> 1][2 * (kt & 1) + 1] = pack_f16x2(e[2], e[3]);
+      }
+    }
+
+    // values: eight tokens a half page and lane
+    Dwords<S::kVDw> v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int tok = 32 * h + 16 * (t >> 2) + 4 * g + (t & 3);
+        v[h][t] = load_dwords<S::kVDw>(vb + tok * D + c * (D / 16));
+        if (masked && 64 * p + tok >= seq) {
+#pragma unroll
+          for (int x = 0; x < S::kVDw; ++x) v[h][t].v[x] = 0;
+        }
+      }
+    // A NaN code that only some rows of the chunk see: the product takes a 0 in
+    // its place, and a second one counts each row's NaNs by dim.
+    bool nans = false;
+    if constexpr (CODE == 0) {
+      if (masked) {
+        uint32_t found = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+#pragma unroll
+            for (int x = 0; x < S::kVDw; ++x) {
+              const uint32_t d = v[h][t].v[x] & 0x7f7f7f7fu;
+              found |= (d + 0x01010101u) & 0x80808080u;  // 0x7f + 1
+            }
+        nans = __any(found != 0);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < S::kVDw; ++x)
+#pragma unroll
+      for (int pr = 0; pr < 2; ++pr) {  // dims 4x + 2 pr, 4x + 2 pr + 1
+        u32x4 f[2][2];                  // [dim][half]
+        u32x4 n[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            uint32_t lo = v[h][2 * t].v[x], hi = v[h][2 * t + 1].v[x];
+            uint32_t pair = __builtin_amdgcn_perm(hi, lo, pr ? 0x07030602u : 0x05010400u);
+            if constexpr (CODE == 1) pair ^= 0x80808080u;
+            if (nans) {
+              const uint32_t bad = ((((pair & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7);  // 1 where NaN
+              pair &= ~(bad * 0xffu);
+              n[0][h][t] = (bad & 1u) * 0x3c00u | ((bad >> 8) & 1u) * 0x3c000000u;
+              n[1][h][t] = ((bad >> 16) & 1u) * 0x3c00u | ((bad >> 24) & 1u) * 0x3c000000u;
+            }
+            f[0][h][t] = pair_to_f16<CODE, false>(pair);
+            f[1][h][t] = pair_to_f16<CODE, true>(pair);
+          }
+#pragma unroll
+        for (int dd = 0; dd < 2; ++dd) {
+          const int j = 4 * x + 2 * pr + dd;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            f32x4 t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const u32x4 wf = {w[mt][h][0], w[mt][h][1], w[mt][h][2], w[mt][h][3]};
+              t = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, f[dd][h]),
+                                                         __builtin_bit_cast(f16x8, wf), t, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[j][mt][i] = __builtin_fmaf(vs, t[i], o[j][mt][i]);
+            if (nans) {
+              f32x4 cnt = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                u32x4 vis;
+#pragma unroll
+                for (int t2 = 0; t2 < 4; ++t2) {
+                  const int key = 64 * p + 32 * h + 16 * (t2 >> 1) + 4 * g + 2 * (t2 & 1);
+                  vis[t2] = (key < sees[mt] ? 0x3c00u : 0u) | (key + 1 < sees[mt] ? 0x3c000000u : 0u);
+                }
+                cnt = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, n[dd][h]),
+                                                             __builtin_bit_cast(f16x8, vis), cnt, 0, 0, 0);
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (cnt[i] > 0.f) o[j][mt][i] = __builtin_nanf("");
+            }
+          }
+        }
+      }
+  }
+
+  // join the four waves: every row's largest reference, then the waves' rows
+  // brought to it
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const float sum = xor_sum(l[mt]);
+    if (g == 0) {
+      lds_m[wave * S::kRows + 16 * mt + c] = m[mt];
+      lds_l[wave * S::kRows + 16 * mt + c] = sum;
+    }
+  }
+  __syncthreads();
+  float by[MT], inv[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    float top = kNegInf;
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, lds_m[w * S::kRows + 16 * mt + c]);
+    by[mt] = m[mt] == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m[mt] - top);
+    float sum = 0.f;
+    for (int w = 0; w < kWaves; ++w) {
+      const float mw = lds_m[w * S::kRows + 16 * mt + c];
+      sum += mw == kNegInf ? 0.f : lds_l[w * S::kRows + 16 * mt + c] * __builtin_amdgcn_exp2f(mw - top);
+    }
+    inv[mt] = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);  // (NaN stays)
+    const int r = row0 + 16 * mt + c;
+    if (wave == 0 && g == 0 && a.lse && r < rows) {
+      const int i = r / a.group, h = hk * a.group + r - i * a.group;
+      const float lse = sum == 0.f ? kNegInf : (top - kWeightShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+      a.lse[((int64_t)b * a.q_chunk + i) * Hq + h] = lse;
+    }
+    by[mt] *= inv[mt];
+  }
+#pragma unroll
+  for (int pass = 0; pass < S::kDims / S::kPass; ++pass) {
+    if (pass) __syncthreads();
+    // the lane's dims [c' kDims + pass * kPass, + kPass) of shares c' = 4g + i
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < S::kPass; j += 4) {
+          f32x4 x;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) x[k] = o[pass * S::kPass + j + k][mt][i] * by[mt];
+          *(f32x4*)(lds_o + (wave * S::kRows + 16 * mt + c) * S::kRowStride + (4 * g + i) * S::kPass + j) = x;
+        }
+    __syncthreads();
+    constexpr int kQuads = 4 * S::kPass;  // 4-float pieces of a row in this pass
+    for (int e = threadIdx.x; e < S::kRows * kQuads; e += 64 * kWaves) {
+      const int rr = e / kQuads, k4 = e - rr * kQuads;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) x += *(const f32x4*)(lds_o + (w * S::kRows + rr) * S::kRowStride + 4 * k4);
+      const int r = row0 + rr;
+      if (r < rows) {
+        const int share = (4 * k4) / S::kPass, d = share * S::kDims + pass * S::kPass + (4 * k4 - share * S::kPass);
+        const int i = r / a.group, h = hk * a.group + r - i * a.group;
+        *(u32x2*)(a.out + (((int64_t)b * a.q_chunk + i) * Hq + h) * D + d) =
+            (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+      }
+    }
+  }
+}
+
+template <int D, int MT, int CODE>
+__global__ __launch_bounds__(64 * kWaves) void gqa_attend_kernel(GqaAttendLaunch a) {
+  using S = Shape<D, MT>;
+  __shared__ __align__(16) float lds_o[kWaves * S::kRows * S::kRowStride];
+  __shared__ float lds_m[kWaves * S::kRows];
+  __shared__ float lds_l[kWaves * S::kRows];
+  const int row_blocks = (a.q_chunk * a.group + S::kRows - 1) / S::kRows;
+  const int tile = blockIdx.x;
+  const int rb = tile % row_blocks, hk = (tile / row_blocks) % a.Hk, b = tile / row_blocks / a.Hk;
+  int seq = a.seq_lens[b];
+  seq = seq < 0 ? 0 : (seq > a.bt_stride * kPage ? a.bt_stride * kPage : seq);
+  attend_pages<D, MT, CODE>(a, b, hk, rb * S::kRows, seq, 0, (seq + kPage - 1) / kPage, lds_o, lds_m, lds_l);
+}
+
+template <int D, int MT, int CODE>
+hipError_t launch_shape(const GqaAttendLaunch& a, hipStream_t s) {
+  const int64_t row_blocks = ((int64_t)a.q_chunk * a.group + 16 * MT - 1) / (16 * MT);
+  hipLaunchKernelGGL((gqa_attend_kernel<D, MT, CODE>), dim3((unsigned)(a.B * a.Hk * row_blocks)), dim3(64 * kWaves), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int CODE>
+hipError_t launch_code(const GqaAttendLaunch& a, hipStream_t s) {
+  const int64_t rows = (int64_t)a.q_chunk * a.group;
+  switch (a.D) {
+    case 64:
+      return rows <= 16 ? launch_shape<64, 1, CODE>(a, s) : rows <= 32 ? launch_shape<64, 2, CODE>(a, s) : launch_shape<64, 4, CODE>(a, s);
+    case 128:
+      return rows <= 16 ? launch_shape<128, 1, CODE>(a, s) : rows <= 32 ? launch_shape<128, 2, CODE>(a, s) : launch_shape<128, 4, CODE>(a, s);
+    default:
+      return rows <= 16 ? launch_shape<256, 1, CODE>(a, s) : launch_shape<256, 2, CODE>(a, s);
+  }
+}
+
+}  // namespace gqa
+}  // namespace splash
