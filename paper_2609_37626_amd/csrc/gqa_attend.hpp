@@ -3,11 +3,15 @@
 //
 // A tile is one request, one KV head and up to 16*MT of its query rows
 // (q_chunk rows times the heads that share the KV head): every K and V byte is
-// read once for all of them.  A workgroup of four waves takes a tile; wave w
-// takes its pages w, w + 4, ..., one page a step, and the four results are
-// joined through LDS.  Nothing else goes through LDS: each operand is loaded
-// from the cache in the layout that its MFMA reads, because the contraction's
-// order is free as long as both operands agree on it.
+// read once for all of them.  The tiles' pages, one tile after the other with
+// kTileCost places in front of each for its fixed work, form one line, which is
+// cut into equal spans, one for each workgroup: long and short histories load
+// the chip alike without a plan, and only the tiles that a cut goes through
+// leave partial results, at most two a workgroup, which a second kernel joins.
+// A workgroup's four waves take the pages of a span's tile in turn, one a step,
+// and join their results through LDS.  Nothing else goes through LDS: each
+// operand is loaded from the cache in the layout that its MFMA reads, because
+// the contraction's order is free as long as both operands agree on it.
 //   QK  S^T[key, row] = K Q^T, v_mfma_f32_16x16x32_bf16.  Lane (g, c), g =
 //       lane / 16, c = lane % 16, holds key c's dims [g D/4, (g+1) D/4) as
 //       contiguous bytes; Q is held the same way.
@@ -40,6 +44,12 @@ constexpr int kWaves = 4;
 constexpr float kWeightShift = 6.f;   // weights are 2^(z - m + 6)
 constexpr float kMoveAt = 8.f;        // the reference moves once a score passes it by this
 constexpr float kNegInf = -__builtin_inff();
+
+// Places of a tile in the line: kTileCost for its fixed work, then its pages.
+// A span is at least kLeastSpan places long: a page and a tile's fixed work
+// for each wave.
+constexpr int kTileCost = 2;
+constexpr int kLeastSpan = 6;
 
 // ---- codes to MFMA operands (exact) --------------------------------------
 
@@ -85,6 +95,12 @@ __device__ __forceinline__ float xor_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+// A row's 1 / sum and LSE from its reference and sum (no key: 0 and -inf; NaN stays).
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+__device__ __forceinline__ float row_lse(float top, float sum) {
+  return sum == 0.f ? kNegInf : (top - kWeightShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+}
+
 // 4-byte pieces as wide as a lane's share of a row.
 template <int N>
 struct Dwords {
@@ -123,10 +139,11 @@ struct Shape {
 };
 
 // One tile's pages [p0, p1) on the four waves.  Writes the normalised rows and
-// their LSE.
+// their LSE, or, with a partial slot (>= 0), the rows over their largest
+// reference, that reference and the weights' sum.
 template <int D, int MT, int CODE>
 __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, int hk, int row0, int seq, int p0, int p1,
-                                             float* lds_o, float* lds_m, float* lds_l) {
+                                             int slot, float* lds_o, float* lds_m, float* lds_l) {
   using S = Shape<D, MT>;
   const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -332,7 +349,7 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
     }
   }
   __syncthreads();
-  float by[MT], inv[MT];
+  float by[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float top = kNegInf;
@@ -343,14 +360,19 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
       const float mw = lds_m[w * S::kRows + 16 * mt + c];
       sum += mw == kNegInf ? 0.f : lds_l[w * S::kRows + 16 * mt + c] * __builtin_amdgcn_exp2f(mw - top);
     }
-    inv[mt] = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);  // (NaN stays)
     const int r = row0 + 16 * mt + c;
-    if (wave == 0 && g == 0 && a.lse && r < rows) {
-      const int i = r / a.group, h = hk * a.group + r - i * a.group;
-      const float lse = sum == 0.f ? kNegInf : (top - kWeightShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
-      a.lse[((int64_t)b * a.q_chunk + i) * Hq + h] = lse;
+    if (slot >= 0) {
+      if (wave == 0 && g == 0) {
+        f32x2* ml = (f32x2*)a.part_ml + (int64_t)slot * S::kRows + 16 * mt + c;
+        *ml = (f32x2){top, sum};
+      }
+    } else {
+      if (wave == 0 && g == 0 && a.lse && r < rows) {
+        const int i = r / a.group, h = hk * a.group + r - i * a.group;
+        a.lse[((int64_t)b * a.q_chunk + i) * Hq + h] = row_lse(top, sum);
+      }
+      by[mt] *= inverse(sum);
     }
-    by[mt] *= inv[mt];
   }
 #pragma unroll
   for (int pass = 0; pass < S::kDims / S::kPass; ++pass) {
@@ -375,8 +397,10 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) x += *(const f32x4*)(lds_o + (w * S::kRows + rr) * S::kRowStride + 4 * k4);
       const int r = row0 + rr;
-      if (r < rows) {
-        const int share = (4 * k4) / S::kPass, d = share * S::kDims + pass * S::kPass + (4 * k4 - share * S::kPass);
+      const int share = (4 * k4) / S::kPass, d = share * S::kDims + pass * S::kPass + (4 * k4 - share * S::kPass);
+      if (slot >= 0) {
+        *(f32x4*)(a.part_out + ((int64_t)slot * S::kRows + rr) * D + d) = x;
+      } else if (r < rows) {
         const int i = r / a.group, h = hk * a.group + r - i * a.group;
         *(u32x2*)(a.out + (((int64_t)b * a.q_chunk + i) * Hq + h) * D + d) =
             (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
@@ -385,38 +409,176 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
   }
 }
 
+__device__ __forceinline__ int history(const GqaAttendLaunch& a, int b) {
+  const int seq = a.seq_lens[b], most = a.bt_stride * kPage;
+  return seq < 0 ? 0 : (seq > most ? most : seq);
+}
+__device__ __forceinline__ int pages_of(int seq) { return (seq + kPage - 1) / kPage; }
+
+// The workgroup's span of the line: every thread sums a few requests' places, a
+// scan over the workgroup gives the line's length and with it the spans, and
+// the thread whose requests hold the span's start finds the request.
+struct Span {
+  int lo, hi;      // places
+  int chunk;       // places of a span
+  int b, b_start;  // the request at lo, and its first place
+};
+__device__ __forceinline__ Span find_span(const GqaAttendLaunch& a, int tiles, int* lds) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int per = (a.B + 64 * kWaves - 1) / (64 * kWaves);
+  int mine = 0;
+  for (int k = 0; k < per; ++k) {
+    const int b = t * per + k;
+    if (b < a.B) mine += tiles * (pages_of(history(a, b)) + kTileCost);
+  }
+  int upto = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int x = __shfl_up(upto, d);
+    if (lane >= d) upto += x;
+  }
+  if (lane == 63) lds[wave] = upto;
+  __syncthreads();
+  int total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) upto += lds[w];
+    total += lds[w];
+  }
+  Span s;
+  s.chunk = max((total + a.workers - 1) / a.workers, kLeastSpan);
+  s.lo = min((int64_t)blockIdx.x * s.chunk, (int64_t)total);
+  s.hi = min((int64_t)s.lo + s.chunk, (int64_t)total);
+  if (s.lo < s.hi && s.lo >= upto - mine && s.lo < upto) {
+    int start = upto - mine;
+    for (int b = t * per;; ++b) {
+      const int next = start + tiles * (pages_of(history(a, b)) + kTileCost);
+      if (s.lo < next) {
+        lds[kWaves] = b;
+        lds[kWaves + 1] = start;
+        break;
+      }
+      start = next;
+    }
+  }
+  __syncthreads();
+  s.b = __builtin_amdgcn_readfirstlane(lds[kWaves]);
+  s.b_start = __builtin_amdgcn_readfirstlane(lds[kWaves + 1]);
+  s.lo = __builtin_amdgcn_readfirstlane(s.lo);
+  s.hi = __builtin_amdgcn_readfirstlane(s.hi);
+  s.chunk = __builtin_amdgcn_readfirstlane(s.chunk);
+  return s;
+}
+
 template <int D, int MT, int CODE>
 __global__ __launch_bounds__(64 * kWaves) void gqa_attend_kernel(GqaAttendLaunch a) {
   using S = Shape<D, MT>;
   __shared__ __align__(16) float lds_o[kWaves * S::kRows * S::kRowStride];
   __shared__ float lds_m[kWaves * S::kRows];
   __shared__ float lds_l[kWaves * S::kRows];
+  __shared__ int lds_span[kWaves + 2];
   const int row_blocks = (a.q_chunk * a.group + S::kRows - 1) / S::kRows;
-  const int tile = blockIdx.x;
-  const int rb = tile % row_blocks, hk = (tile / row_blocks) % a.Hk, b = tile / row_blocks / a.Hk;
-  int seq = a.seq_lens[b];
-  seq = seq < 0 ? 0 : (seq > a.bt_stride * kPage ? a.bt_stride * kPage : seq);
-  attend_pages<D, MT, CODE>(a, b, hk, rb * S::kRows, seq, 0, (seq + kPage - 1) / kPage, lds_o, lds_m, lds_l);
+  const int tiles = a.Hk * row_blocks;  // of a request
+  const Span span = find_span(a, tiles, lds_span);
+  int4 joined = {-1, 0, 0, 0};  // the tile that this workgroup has the first part of
+  int b = span.b, b_start = span.b_start;
+  for (int at = span.lo; at < span.hi;) {
+    const int seq = history(a, b), pages = pages_of(seq), cost = pages + kTileCost;
+    const int tile = (at - b_start) / cost, start = b_start + tile * cost;
+    const int hk = tile / row_blocks, rb = tile - hk * row_blocks;
+    const int p0 = max(at - start - kTileCost, 0), p1 = min(span.hi - start - kTileCost, pages);
+    // (a tile without a page belongs to the span of its first place)
+    if (p0 < p1 || (pages == 0 && at == start)) {
+      int slot = -1;
+      if (p0 > 0) {
+        slot = 2 * blockIdx.x;
+      } else if (p1 < pages) {
+        slot = 2 * blockIdx.x + 1;
+        joined = {b, hk, rb, (start + kTileCost + pages - 1) / span.chunk - (int)blockIdx.x + 1};
+      }
+      attend_pages<D, MT, CODE>(a, b, hk, rb * S::kRows, seq, p0, p1, slot, lds_o, lds_m, lds_l);
+      __syncthreads();
+    }
+    at = start + cost;
+    if (tile == tiles - 1) {
+      ++b;
+      b_start = at;
+    }
+  }
+  if (threadIdx.x == 0) a.joined[blockIdx.x] = joined;
+}
+
+// Joins the parts of the tile whose first part workgroup blockIdx.x of the
+// attend kernel has, if any: one wave per row.  The parts lie in slots 2w + 1,
+// 2(w + 1), 2(w + 2), ...; lanes take 4 dims each, 64 / (D / 4) parts at a time.
+template <int D, int MT>
+__global__ __launch_bounds__(64 * kWaves) void gqa_join_kernel(GqaAttendLaunch a) {
+  using S = Shape<D, MT>;
+  const int w = blockIdx.x, lane = threadIdx.x & 63;
+  const int4 tile = a.joined[w];
+  if (tile.x < 0) return;
+  const int rr = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = tile.z * S::kRows + rr;
+  if (r >= a.q_chunk * a.group) return;
+  const int parts = tile.w;
+  const auto slot = [&](int p) { return (int64_t)(p == 0 ? 2 * w + 1 : 2 * (w + p)); };
+  const f32x2* ml = (const f32x2*)a.part_ml;
+  float top = kNegInf;
+  for (int p = lane; p < parts; p += 64) top = fmaxf(top, ml[slot(p) * S::kRows + rr][0]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  constexpr int kLanes = D / 4, kSide = 64 / kLanes;  // lanes of a row; parts side by side
+  const int d = 4 * (lane % kLanes);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+#pragma unroll 4
+  for (int p = lane / kLanes; p < parts; p += kSide) {
+    const int64_t at = slot(p) * S::kRows + rr;
+    const f32x2 v = ml[at];
+    const f32x4 x = *(const f32x4*)(a.part_out + at * D + d);
+    if (v[0] != kNegInf) {
+      const float by = __builtin_amdgcn_exp2f(v[0] - top);
+      sum += v[1] * by;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(x[i], by, o[i]);
+    }
+  }
+#pragma unroll
+  for (int x = kLanes; x < 64; x <<= 1) {
+    sum += __shfl_xor(sum, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], x);
+  }
+  const int i = r / a.group, h = tile.y * a.group + r - i * a.group;
+  const int64_t row = ((int64_t)tile.x * a.q_chunk + i) * (a.Hk * a.group) + h;
+  if (lane < kLanes) {
+    const float inv = inverse(sum);
+    *(u32x2*)(a.out + row * D + d) = (u32x2){pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+    if (lane == 0 && a.lse) a.lse[row] = row_lse(top, sum);
+  }
 }
 
 template <int D, int MT, int CODE>
-hipError_t launch_shape(const GqaAttendLaunch& a, hipStream_t s) {
-  const int64_t row_blocks = ((int64_t)a.q_chunk * a.group + 16 * MT - 1) / (16 * MT);
-  hipLaunchKernelGGL((gqa_attend_kernel<D, MT, CODE>), dim3((unsigned)(a.B * a.Hk * row_blocks)), dim3(64 * kWaves), 0, s, a);
+hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
+  using S = Shape<D, MT>;
+  const int64_t row_blocks = ((int64_t)a.q_chunk * a.group + S::kRows - 1) / S::kRows;
+  // no more workgroups than the longest histories would fill
+  const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * (a.bt_stride + kTileCost) + kLeastSpan - 1) / kLeastSpan;
+  if (a.workers > most) a.workers = (int32_t)most;
+  hipLaunchKernelGGL((gqa_attend_kernel<D, MT, CODE>), dim3(a.workers), dim3(64 * kWaves), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((gqa_join_kernel<D, MT>), dim3(a.workers, S::kRows / kWaves), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
 
+// Rows of a tile, by the rows that share a KV head: the fewest that hold them,
+// at most 64 (32 at 256 dims, whose accumulators would not fit).
 template <int CODE>
 hipError_t launch_code(const GqaAttendLaunch& a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.q_chunk * a.group;
-  switch (a.D) {
-    case 64:
-      return rows <= 16 ? launch_shape<64, 1, CODE>(a, s) : rows <= 32 ? launch_shape<64, 2, CODE>(a, s) : launch_shape<64, 4, CODE>(a, s);
-    case 128:
-      return rows <= 16 ? launch_shape<128, 1, CODE>(a, s) : rows <= 32 ? launch_shape<128, 2, CODE>(a, s) : launch_shape<128, 4, CODE>(a, s);
-    default:
-      return rows <= 16 ? launch_shape<256, 1, CODE>(a, s) : launch_shape<256, 2, CODE>(a, s);
-  }
+  const int mt = gqa_row_tiles(a.D, (int64_t)a.q_chunk * a.group);
+  if (a.D == 64) return mt == 1 ? launch_shape<64, 1, CODE>(a, s) : mt == 2 ? launch_shape<64, 2, CODE>(a, s) : launch_shape<64, 4, CODE>(a, s);
+  if (a.D == 128) return mt == 1 ? launch_shape<128, 1, CODE>(a, s) : mt == 2 ? launch_shape<128, 2, CODE>(a, s) : launch_shape<128, 4, CODE>(a, s);
+  return mt == 1 ? launch_shape<256, 1, CODE>(a, s) : launch_shape<256, 2, CODE>(a, s);
 }
 
 }  // namespace gqa

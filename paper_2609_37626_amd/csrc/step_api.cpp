@@ -51,6 +51,20 @@ int check_gqa_cache(const void* k_pages, const void* v_pages, const float* k_sca
   return SPLASH_OK;
 }
 
+struct GqaLayout {
+  size_t part_ml, part_out, total;  // the joined tiles' records come first
+};
+
+GqaLayout gqa_layout(const splash_gqa_desc* d, int32_t q_chunk) {
+  const int64_t rows = 16 * gqa_row_tiles(d->head_dim, (int64_t)q_chunk * (d->num_heads / d->num_kv_heads));
+  const size_t slots = 2 * (size_t)kGqaMaxWorkers * rows;
+  GqaLayout l;
+  l.part_ml = sizeof(int4) * kGqaMaxWorkers;
+  l.part_out = l.part_ml + slots * 2 * sizeof(float);
+  l.total = l.part_out + slots * d->head_dim * sizeof(float);
+  return l;
+}
+
 }  // namespace
 
 extern "C" {
@@ -153,8 +167,12 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
 }
 
 size_t splash_gqa_workspace_size(const splash_gqa_desc* desc, int32_t q_chunk) {
-  if (validate_gqa(desc) != SPLASH_OK || q_chunk < 1) return 0;
-  return 256;
+  if (validate_gqa(desc) != SPLASH_OK) return 0;
+  if (q_chunk < 1) {
+    fail(SPLASH_ERR_INVALID_ARGUMENT, "q_chunk must be >= 1 (got %d)", q_chunk);
+    return 0;
+  }
+  return gqa_layout(desc, q_chunk).total;
 }
 
 int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, const float* k_scales,
@@ -179,9 +197,9 @@ int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, c
   const int64_t tiles = row_blocks > (1 << 20) ? INT64_MAX : (int64_t)desc->batch * desc->num_kv_heads * row_blocks;
   if (tiles > (1 << 30) || tiles * ((int64_t)desc->max_pages_per_seq + 8) > (1 << 30))
     return fail(SPLASH_ERR_UNSUPPORTED, "batch * num_kv_heads * row blocks * pages passes 2^30");
-  const size_t need = splash_gqa_workspace_size(desc, q_chunk);
-  if (ws_bytes < need)
-    return fail(SPLASH_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, need %zu", ws_bytes, need);
+  const GqaLayout layout = gqa_layout(desc, q_chunk);
+  if (ws_bytes < layout.total)
+    return fail(SPLASH_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes, need %zu", ws_bytes, layout.total);
   GqaAttendLaunch a = {};
   a.q = static_cast<const uint16_t*>(q);
   a.k_pages = static_cast<const uint8_t*>(k_pages);
@@ -200,6 +218,12 @@ int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, c
   a.bt_stride = desc->max_pages_per_seq;
   a.num_pages = desc->num_pages;
   a.code_type = desc->code_type;
+  char* ws = static_cast<char*>(workspace);
+  a.joined = reinterpret_cast<int4*>(ws);
+  a.part_ml = reinterpret_cast<float*>(ws + layout.part_ml);
+  a.part_out = reinterpret_cast<float*>(ws + layout.part_out);
+  const int32_t cus = splash_device_workers();
+  a.workers = 2 * cus < kGqaMaxWorkers ? 2 * cus : kGqaMaxWorkers;
   a.scale_log2 = desc->softmax_scale * 1.44269504088896340736f;
   const hipError_t e = launch_gqa_attend(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SPLASH_OK : hip_fail(e, "gqa attend launch");
