@@ -101,14 +101,22 @@ __device__ __forceinline__ float row_lse(float top, float sum) {
   return sum == 0.f ? kNegInf : (top - kWeightShift + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
+// (uniform: through the scalar cache, so that it waits for no vector load)
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
 // 4-byte pieces as wide as a lane's share of a row.
 template <int N>
 struct Dwords {
   uint32_t v[N];
 };
+// `at` is uniform and `lane` the lane's own offset, so that the address takes one register.
 template <int N>
-__device__ __forceinline__ Dwords<N> load_dwords(const uint8_t* p) {
+__device__ __forceinline__ Dwords<N> load_dwords(const uint8_t* at, uint32_t lane) {
   Dwords<N> r;
+  const uint8_t* p = at + lane;
   if constexpr (N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < N / 4; ++i) {
@@ -133,10 +141,31 @@ struct Shape {
   static constexpr int kKDw = D / 16;       // dwords of a lane's share of a K row (D/4 bytes)
   static constexpr int kVDw = D / 64;       // dwords of a lane's share of a V row (D/16 bytes)
   static constexpr int kDims = D / 16;      // dims of a lane's share, = MFMA row groups of O^T
+  static constexpr int kPerCu = D * MT <= 256 && D < 256 ? 2 : 1;  // workgroups on a CU: 256 registers a wave, or 512
   // the four waves' results are joined kPass dims of each share at a time, in at most 64 KB
   static constexpr int kPass = (kWaves * kRows * D * 4 <= 65536) ? kDims : 65536 / (kWaves * kRows * 64);
   static constexpr int kRowStride = 16 * kPass + 4;  // floats, padded by a 16-byte bank group
 };
+
+// 1 in every byte that is an E4M3 NaN (0x7f, 0xff).
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t d) { return (((d & 0x7f7f7f7fu) + 0x01010101u) >> 7) & 0x01010101u; }
+
+// NaN codes of a page that some rows see in part: each lane looks through V for
+// its own outputs; bit 4 j + i of `hit` is dim group j, element i.  (Rare, so
+// V is read again, byte by byte, and the loop takes few registers.)
+template <int D, int MT>
+__device__ __forceinline__ void nan_rows(const uint8_t* vb, int key0, int seq, const int (&sees)[MT], uint64_t (&hit)[MT]) {
+  const int g = (threadIdx.x & 63) >> 4;
+  const int end = min(kPage, seq - key0);
+#pragma unroll 1
+  for (int tok = 0; tok < end; ++tok)
+#pragma unroll 1
+    for (int e = 0; e < D / 4; ++e)
+      if ((vb[tok * D + (4 * g + (e & 3)) * (D / 16) + (e >> 2)] & 0x7f) == 0x7f)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          if (key0 + tok < sees[mt]) hit[mt] |= 1ull << e;
+}
 
 // One tile's pages [p0, p1) on the four waves.  Writes the normalised rows and
 // their LSE, or, with a partial slot (>= 0), the rows over their largest
@@ -173,41 +202,76 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
 
   f32x4 o[S::kDims][MT];
   float m[MT], l[MT];
+  uint64_t hit[MT];  // NaN outputs, see nan_rows()
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
+    hit[mt] = 0;
     m[mt] = kNegInf;
     l[mt] = 0.f;
 #pragma unroll
     for (int j = 0; j < S::kDims; ++j) o[j][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
 
+  // The wave's pages p0 + wave, + kWaves, ...: while a page is worked on, its V
+  // is in flight from before QK and the next page's K from after it, and the
+  // block-table entry of the page after that is on its way.  A place whose entry
+  // lies outside the pool reads page 0, all of it masked; past the last page the
+  // last one is read again.
   const int32_t* bt = a.block_table + (int64_t)b * a.bt_stride;
-  for (int p = p0 + wave; p < p1; p += kWaves) {
-    const int page = bt[p];
-    if ((unsigned)page >= (unsigned)a.num_pages) continue;
-    const int64_t block = (int64_t)page * a.Hk + hk;
+  const auto entry = [&](int p) { return scalar_load(bt + min(p, p1 - 1)); };
+  const auto block_of = [&](int page) {
+    return (int64_t)((unsigned)page < (unsigned)a.num_pages ? page : 0) * a.Hk + hk;
+  };
+  const uint32_t k_lane = c * D + g * (D / 4), v_lane = 4 * g * D + c * (D / 16);
+  Dwords<S::kKDw> k[4];
+  const auto load_k = [&](int64_t block) {
     const uint8_t* kb = a.k_pages + block * (kPage * D);
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) k[kt] = load_dwords<S::kKDw>(kb + 16 * kt * D, k_lane);
+  };
+  int p = p0 + wave, page = entry(p), next = entry(p + kWaves);
+  int64_t block = block_of(page);
+  float ks = scalar_load(a.k_scales + block) * a.scale_log2, vs = scalar_load(a.v_scales + block);
+  if (p < p1) load_k(block);
+  for (; p < p1; p += kWaves) {
+    const bool held = (unsigned)page < (unsigned)a.num_pages;
+    const bool masked = !held || 64 * p + 64 > all_see;
+
+    // values: eight tokens a half page and lane
     const uint8_t* vb = a.v_pages + block * (kPage * D);
-    const float ks = a.k_scales[block] * a.scale_log2, vs = a.v_scales[block];
-    const bool masked = 64 * p + 64 > all_see;
+    Dwords<S::kVDw> v[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int t = 0; t < 8; ++t)
+        v[h][t] = load_dwords<S::kVDw>(vb + (32 * h + 16 * (t >> 2) + (t & 3)) * D, v_lane);
+    const int after = entry(p + 2 * kWaves);
+    const int64_t next_block = block_of(next);
+    const float next_ks = scalar_load(a.k_scales + next_block) * a.scale_log2, next_vs = scalar_load(a.v_scales + next_block);
+    __builtin_amdgcn_sched_barrier(0);
 
     // scores
     f32x4 z[4][MT];
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
-      const Dwords<S::kKDw> k = load_dwords<S::kKDw>(kb + (16 * kt + c) * D + g * (D / 4));
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) z[kt][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < S::kSteps; ++s) {
-        const bf16x8 kf = codes_to_bf16<CODE>(k.v[2 * s], k.v[2 * s + 1]);
+        const bf16x8 kf = codes_to_bf16<CODE>(k[kt].v[2 * s], k[kt].v[2 * s + 1]);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
           z[kt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[mt][s], z[kt][mt], 0, 0, 0);
       }
+      if (kt & 1) __builtin_amdgcn_sched_barrier(0);  // (or all of K is converted ahead, in twice its registers)
+    }
+    load_k(next_block);
+    __builtin_amdgcn_sched_barrier(0);
+
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) z[kt][mt] *= ks;
-    }
     if (masked) {
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
@@ -215,7 +279,7 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (64 * p + 16 * kt + 4 * g + i >= sees[mt]) z[kt][mt][i] = kNegInf;
+            if (!held || 64 * p + 16 * kt + 4 * g + i >= sees[mt]) z[kt][mt][i] = kNegInf;
     }
 
     // weights
@@ -249,35 +313,27 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
       }
     }
 
-    // values: eight tokens a half page and lane
-    Dwords<S::kVDw> v[2][8];
+    // Codes of places that no row sees count as 0, and so do NaN codes of a
+    // page that some row sees in part; nan_rows() gives those to their rows.
+    if (masked) {
+      const int end = held ? seq - 64 * p : 0;
+      uint32_t found = 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int tok = 32 * h + 16 * (t >> 2) + 4 * g + (t & 3);
-        v[h][t] = load_dwords<S::kVDw>(vb + tok * D + c * (D / 16));
-        if (masked && 64 * p + tok >= seq) {
+        for (int t = 0; t < 8; ++t)
 #pragma unroll
-          for (int x = 0; x < S::kVDw; ++x) v[h][t].v[x] = 0;
-        }
-      }
-    // A NaN code that only some rows of the chunk see: the product takes a 0 in
-    // its place, and a second one counts each row's NaNs by dim.
-    bool nans = false;
-    if constexpr (CODE == 0) {
-      if (masked) {
-        uint32_t found = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int x = 0; x < S::kVDw; ++x) {
-              const uint32_t d = v[h][t].v[x] & 0x7f7f7f7fu;
-              found |= (d + 0x01010101u) & 0x80808080u;  // 0x7f + 1
+          for (int x = 0; x < S::kVDw; ++x) {
+            uint32_t& d = v[h][t].v[x];
+            if (32 * h + 16 * (t >> 2) + 4 * g + (t & 3) >= end) d = 0;
+            if constexpr (CODE == 0) {
+              const uint32_t bad = nan_bytes(d);
+              d &= ~(bad * 255u);
+              found |= bad;
             }
-        nans = __any(found != 0);
+          }
+      if constexpr (CODE == 0) {
+        if (__any(found != 0)) nan_rows<D, MT>(vb, 64 * p, held ? seq : 0, sees, hit);
       }
     }
 #pragma unroll
@@ -285,20 +341,12 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
 #pragma unroll
       for (int pr = 0; pr < 2; ++pr) {  // dims 4x + 2 pr, 4x + 2 pr + 1
         u32x4 f[2][2];                  // [dim][half]
-        u32x4 n[2][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            uint32_t lo = v[h][2 * t].v[x], hi = v[h][2 * t + 1].v[x];
-            uint32_t pair = __builtin_amdgcn_perm(hi, lo, pr ? 0x07030602u : 0x05010400u);
+            uint32_t pair = __builtin_amdgcn_perm(v[h][2 * t + 1].v[x], v[h][2 * t].v[x], pr ? 0x07030602u : 0x05010400u);
             if constexpr (CODE == 1) pair ^= 0x80808080u;
-            if (nans) {
-              const uint32_t bad = ((((pair & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7);  // 1 where NaN
-              pair &= ~(bad * 0xffu);
-              n[0][h][t] = (bad & 1u) * 0x3c00u | ((bad >> 8) & 1u) * 0x3c000000u;
-              n[1][h][t] = ((bad >> 16) & 1u) * 0x3c00u | ((bad >> 24) & 1u) * 0x3c000000u;
-            }
             f[0][h][t] = pair_to_f16<CODE, false>(pair);
             f[1][h][t] = pair_to_f16<CODE, true>(pair);
           }
@@ -316,26 +364,26 @@ __device__ __forceinline__ void attend_pages(const GqaAttendLaunch& a, int b, in
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[j][mt][i] = __builtin_fmaf(vs, t[i], o[j][mt][i]);
-            if (nans) {
-              f32x4 cnt = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                u32x4 vis;
-#pragma unroll
-                for (int t2 = 0; t2 < 4; ++t2) {
-                  const int key = 64 * p + 32 * h + 16 * (t2 >> 1) + 4 * g + 2 * (t2 & 1);
-                  vis[t2] = (key < sees[mt] ? 0x3c00u : 0u) | (key + 1 < sees[mt] ? 0x3c000000u : 0u);
-                }
-                cnt = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, n[dd][h]),
-                                                             __builtin_bit_cast(f16x8, vis), cnt, 0, 0, 0);
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (cnt[i] > 0.f) o[j][mt][i] = __builtin_nanf("");
-            }
           }
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
+    page = next;
+    next = after;
+    block = next_block;
+    ks = next_ks;
+    vs = next_vs;
+  }
+
+  if constexpr (CODE == 0) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+      if (__any(hit[mt] != 0))
+#pragma unroll
+        for (int j = 0; j < S::kDims; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (hit[mt] >> (4 * j + i) & 1) o[j][mt][i] = __builtin_nanf("");
   }
 
   // join the four waves: every row's largest reference, then the waves' rows
@@ -470,7 +518,7 @@ __device__ __forceinline__ Span find_span(const GqaAttendLaunch& a, int tiles, i
 }
 
 template <int D, int MT, int CODE>
-__global__ __launch_bounds__(64 * kWaves) void gqa_attend_kernel(GqaAttendLaunch a) {
+__global__ __launch_bounds__(64 * kWaves, (Shape<D, MT>::kPerCu)) void gqa_attend_kernel(GqaAttendLaunch a) {
   using S = Shape<D, MT>;
   __shared__ __align__(16) float lds_o[kWaves * S::kRows * S::kRowStride];
   __shared__ float lds_m[kWaves * S::kRows];
@@ -482,7 +530,7 @@ __global__ __launch_bounds__(64 * kWaves) void gqa_attend_kernel(GqaAttendLaunch
   int4 joined = {-1, 0, 0, 0};  // the tile that this workgroup has the first part of
   int b = span.b, b_start = span.b_start;
   for (int at = span.lo; at < span.hi;) {
-    const int seq = history(a, b), pages = pages_of(seq), cost = pages + kTileCost;
+    const int seq = __builtin_amdgcn_readfirstlane(history(a, b)), pages = pages_of(seq), cost = pages + kTileCost;
     const int tile = (at - b_start) / cost, start = b_start + tile * cost;
     const int hk = tile / row_blocks, rb = tile - hk * row_blocks;
     const int p0 = max(at - start - kTileCost, 0), p1 = min(span.hi - start - kTileCost, pages);
@@ -561,6 +609,7 @@ template <int D, int MT, int CODE>
 hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
   using S = Shape<D, MT>;
   const int64_t row_blocks = ((int64_t)a.q_chunk * a.group + S::kRows - 1) / S::kRows;
+  a.workers = a.workers * S::kPerCu < kGqaMaxWorkers ? a.workers * S::kPerCu : kGqaMaxWorkers;
   // no more workgroups than the longest histories would fill
   const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * (a.bt_stride + kTileCost) + kLeastSpan - 1) / kLeastSpan;
   if (a.workers > most) a.workers = (int32_t)most;

@@ -222,8 +222,7 @@ int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, c
   a.joined = reinterpret_cast<int4*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + layout.part_ml);
   a.part_out = reinterpret_cast<float*>(ws + layout.part_out);
-  const int32_t cus = splash_device_workers();
-  a.workers = 2 * cus < kGqaMaxWorkers ? 2 * cus : kGqaMaxWorkers;
+  a.workers = splash_device_workers();
   a.scale_log2 = desc->softmax_scale * 1.44269504088896340736f;
   const hipError_t e = launch_gqa_attend(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SPLASH_OK : hip_fail(e, "gqa attend launch");
