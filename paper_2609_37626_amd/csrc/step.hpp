@@ -70,7 +70,7 @@ struct GqaAttendLaunch {
   int32_t B, Hk, group, D, q_chunk, bt_stride, num_pages, code_type;
   float scale_log2;  // softmax_scale * log2(e)
   int32_t workers;   // compute units; the launch makes it workgroups, at most kGqaMaxWorkers
-  // workspace: two partial results per workgroup, of 16 gqa_row_tiles() rows,
+  // workspace: two partial results per workgroup, of gqa_tile_rows() rows,
   // and {request, KV head, row block, parts} of the tile it begins (request -1: none)
   int4* joined;      // [workers]
   float* part_ml;    // [2 workers, rows, 2] reference and sum of a row
@@ -79,8 +79,11 @@ struct GqaAttendLaunch {
 
 constexpr int32_t kGqaMaxWorkers = 512;
 
-// 16-row MFMA tiles of a workgroup, for `rows` query rows per KV head.
-inline int32_t gqa_row_tiles(int32_t D, int64_t rows) { return rows <= 16 ? 1 : (rows <= 32 || D == 256) ? 2 : 4; }
+// Query rows of a tile, for `rows` of them per KV head: the fewest that hold
+// them, at most 128 (64 at 256 dims, whose accumulators take twice the registers).
+inline int32_t gqa_tile_rows(int32_t D, int64_t rows) {
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : (rows <= 64 || D == 256) ? 64 : 128;
+}
 
 hipError_t launch_step_tables(const TablesLaunch& p, hipStream_t s);
 hipError_t launch_rope(const RopeLaunch& p, hipStream_t s);

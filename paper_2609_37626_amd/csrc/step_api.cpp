@@ -56,7 +56,7 @@ struct GqaLayout {
 };
 
 GqaLayout gqa_layout(const splash_gqa_desc* d, int32_t q_chunk) {
-  const int64_t rows = 16 * gqa_row_tiles(d->head_dim, (int64_t)q_chunk * (d->num_heads / d->num_kv_heads));
+  const int64_t rows = gqa_tile_rows(d->head_dim, (int64_t)q_chunk * (d->num_heads / d->num_kv_heads));
   const size_t slots = 2 * (size_t)kGqaMaxWorkers * rows;
   GqaLayout l;
   l.part_ml = sizeof(int4) * kGqaMaxWorkers;

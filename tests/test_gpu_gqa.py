@@ -82,6 +82,14 @@ def test_attend_skips_pages_outside_the_pool():
     check(p)
     p.lens = np.array([10 ** 9, -5, 60], dtype=np.int32)  # past the table row, negative
     check(p)
+    # the places of skipped pages read nothing of the pool's first page either
+    p = Attend([300, 500, 60], 2, 4, 64, 2, False, seed=12)
+    p.table[p.table == 0] = -1
+    p.table[0, 2] = -1
+    p.poison()
+    p.ks[0] = p.vs[0] = np.nan
+    p.k[0] = p.v[0] = 0xFF
+    check(p)
 
 
 def test_attend_is_deterministic_and_independent_of_placement():
