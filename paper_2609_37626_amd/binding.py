@@ -360,33 +360,45 @@ def _refuse(message: str):
     raise SplashError(SPLASH_ERR_INVALID_ARGUMENT, message)
 
 
-def _device_of(first, **tensors) -> int:
-    """The device of `first`; every tensor is on it, contiguous and of its type."""
-    dev = first.get_device()
+_I32T = _F32T = _BF16T = None  # torch's types, and the call that names the device (set by _types)
+_device = None
+
+
+def _types():
+    global _I32T, _F32T, _BF16T, _device
+    import torch
+    _I32T, _F32T, _BF16T, _device = torch.int32, torch.float32, torch.bfloat16, torch._C._cuda_getDevice
+
+
+def _refuse_tensors(dev: int, **tensors):
+    """Says which tensor is not of its type and shape, contiguous and on the device (name=(tensor, types, shape); a
+    shape of None is any).  The calls find that one is by one condition over all of them, in about 2 us."""
     if dev < 0:
         _refuse("tensors must be on the GPU")
-    for name, (t, dtype, shape) in tensors.items():
+    for name, (t, dtypes, shape) in tensors.items():
         if t is None:
             continue
-        if t.dtype not in dtype:
-            _refuse(f"{name} must be {' or '.join(str(d) for d in dtype)} (got {t.dtype})")
-        if shape is not None and tuple(t.shape) != shape:
-            _refuse(f"{name} must have shape {shape} (got {tuple(t.shape)})")
+        if t.dtype not in dtypes:
+            _refuse(f"{name} must be {' or '.join(str(d) for d in dtypes)} (got {t.dtype})")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            _refuse(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
         if not t.is_contiguous():
             _refuse(f"{name} must be contiguous")
         if t.get_device() != dev:
             _refuse(f"{name} is on another device")
-    return dev
+    _refuse("tensors do not match")
 
 
-def _on_device(dev: int, call, stream) -> None:
-    """call(stream handle) with `dev` current."""
-    import torch
-    if torch._C._cuda_getDevice() == dev:
-        _check(call(_stream(stream)))
+def _on_device(dev: int, fn, args, stream) -> None:
+    """fn(*args, stream handle) with `dev` current."""
+    if _device() == dev:
+        status = fn(*args, _stream(stream))
     else:
+        import torch
         with torch.cuda.device(dev):
-            _check(call(_stream(stream)))
+            status = fn(*args, _stream(stream))
+    if status != SPLASH_OK:
+        _check(status)
 
 
 def make_gqa_desc(batch: int, num_heads: int, num_kv_heads: int, head_dim: int, max_pages_per_seq: int, num_pages: int,
@@ -441,87 +453,130 @@ def make_rope(rot_dim: int, inv_freq, pair_axis=None, num_axes: Optional[int] = 
 def splash_step_tables(seq_lens, q_chunk: int, free_pages, taken_in, taken_out, block_table, num_pages: int, new_indptr,
                        slots, positions, requests, new_lens=None, stream=None) -> None:
     """Pages, slots and positions of the step's new tokens (new_lens[b], or q_chunk of every request)."""
-    import torch
-    i32 = (torch.int32,)
-    b, rows = seq_lens.numel(), slots.numel()
-    dev = _device_of(seq_lens, seq_lens=(seq_lens, i32, (b,)), new_lens=(new_lens, i32, (b,)),
-                     free_pages=(free_pages, i32, None), taken_in=(taken_in, i32, (2,)), taken_out=(taken_out, i32, (2,)),
-                     block_table=(block_table, i32, (b, block_table.shape[-1])), new_indptr=(new_indptr, i32, (b + 1,)),
-                     slots=(slots, i32, (rows,)), positions=(positions, i32, (rows,)), requests=(requests, i32, (rows,)))
-    _on_device(dev, lambda s: lib().splash_step_tables(
-        _ptr(seq_lens), _ptr(new_lens), q_chunk, b, _ptr(free_pages), free_pages.numel(), _ptr(taken_in), _ptr(taken_out),
-        _ptr(block_table), block_table.shape[-1], num_pages, rows, _ptr(new_indptr), _ptr(slots), _ptr(positions),
-        _ptr(requests), s), stream)
+    if _device is None:
+        _types()
+    i32 = _I32T
+    b, rows, width, dev = seq_lens.numel(), slots.numel(), block_table.shape[-1], seq_lens.get_device()
+    new = seq_lens if new_lens is None else new_lens
+    if not (seq_lens.dtype is i32 and new.dtype is i32 and free_pages.dtype is i32 and taken_in.dtype is i32
+            and taken_out.dtype is i32 and block_table.dtype is i32 and new_indptr.dtype is i32 and slots.dtype is i32
+            and positions.dtype is i32 and requests.dtype is i32
+            and new.numel() == b and taken_in.numel() == 2 and taken_out.numel() == 2 and block_table.shape == (b, width)
+            and new_indptr.numel() == b + 1 and positions.numel() == rows and requests.numel() == rows
+            and seq_lens.is_contiguous() and new.is_contiguous() and free_pages.is_contiguous() and taken_in.is_contiguous()
+            and taken_out.is_contiguous() and block_table.is_contiguous() and new_indptr.is_contiguous()
+            and slots.is_contiguous() and positions.is_contiguous() and requests.is_contiguous()
+            and 0 <= dev == new.get_device() == free_pages.get_device() == taken_in.get_device() == taken_out.get_device()
+            == block_table.get_device() == new_indptr.get_device() == slots.get_device() == positions.get_device()
+            == requests.get_device()):
+        t = (i32,)
+        _refuse_tensors(dev, seq_lens=(seq_lens, t, (b,)), new_lens=(new_lens, t, (b,)), free_pages=(free_pages, t, None),
+                        taken_in=(taken_in, t, (2,)), taken_out=(taken_out, t, (2,)), block_table=(block_table, t, (b, width)),
+                        new_indptr=(new_indptr, t, (b + 1,)), slots=(slots, t, (rows,)), positions=(positions, t, (rows,)),
+                        requests=(requests, t, (rows,)))
+    _on_device(dev, lib().splash_step_tables, (
+        seq_lens.data_ptr(), None if new_lens is None else new.data_ptr(), q_chunk, b, free_pages.data_ptr(),
+        free_pages.numel(), taken_in.data_ptr(), taken_out.data_ptr(), block_table.data_ptr(), width, num_pages, rows,
+        new_indptr.data_ptr(), slots.data_ptr(), positions.data_ptr(), requests.data_ptr()), stream)
 
 
 def _rope_view(view: RopeView, x, y, tokens: int, rot_dim: int, dev: int) -> None:
-    import torch
-    for name, t in (("x", x), ("out", y)):
-        if t.dtype != torch.bfloat16 or t.get_device() != dev:
-            _refuse(f"{name} must be bf16 on the positions' device")
-        if t.dim() != 3 or t.shape[0] != tokens or t.shape[1] != x.shape[1] or t.shape[2] != rot_dim or t.stride(2) != 1:
-            _refuse(f"{name} must be [{tokens}, heads, {rot_dim}] with the last dimension dense (got {tuple(t.shape)}, "
-                    f"strides {t.stride()})")
-    view.x, view.y, view.num_heads = x.data_ptr(), y.data_ptr(), x.shape[1]
-    view.x_token_stride, view.x_head_stride, _ = x.stride()
-    view.y_token_stride, view.y_head_stride, _ = y.stride()
+    shape = x.shape
+    xs, ys = x.stride(), y.stride()
+    if not (x.dtype is _BF16T and y.dtype is _BF16T and x.get_device() == dev == y.get_device() and len(shape) == 3
+            and shape == y.shape and shape[0] == tokens and shape[2] == rot_dim and xs[2] == 1 == ys[2]):
+        _refuse(f"x and out must be bf16 [{tokens}, heads, {rot_dim}] on the positions' device, the last dimension dense "
+                f"(got {x.dtype}, {y.dtype}, {tuple(shape)}, {tuple(y.shape)}, strides {xs}, {ys})")
+    view.x = x.data_ptr()
+    view.y = y.data_ptr()
+    view.num_heads = shape[1]
+    view.x_token_stride, view.x_head_stride, _ = xs
+    view.y_token_stride, view.y_head_stride, _ = ys
 
 
 def splash_rope(x, positions, rope: RopeDesc, out=None, x2=None, out2=None, stream=None) -> None:
     """Turns x (and x2) [tokens, heads, rot_dim], views of any token and head stride, by positions [tokens] or
     [axes, tokens] into out (None: in place)."""
-    import torch
-    pos = positions if positions.dim() == 2 else positions[None]
-    if pos.dim() != 2 or pos.shape[0] != rope.num_axes or pos.dtype != torch.int32 or (pos.shape[1] > 1 and pos.stride(1) != 1):
-        _refuse(f"positions must be int32 [{rope.num_axes}, tokens], dense along the tokens")
-    dev, n = pos.get_device(), pos.shape[1]
-    if dev < 0:
-        _refuse("tensors must be on the GPU")
+    if _device is None:
+        _types()
+    shape, strides, dev = positions.shape, positions.stride(), positions.get_device()
+    axes, n = (1, shape[0]) if len(shape) == 1 else shape if len(shape) == 2 else (0, 0)
+    if axes != rope.num_axes or positions.dtype is not _I32T or (n > 1 and strides[-1] != 1) or dev < 0:
+        _refuse(f"positions must be int32 [{rope.num_axes}, tokens] on the GPU, dense along the tokens")
     views = (RopeView * 2)()
-    _rope_view(views[0], x, x if out is None else out, n, rope.rot_dim, dev)
+    rot = rope.rot_dim
+    _rope_view(views[0], x, x if out is None else out, n, rot, dev)
     if x2 is not None:
-        _rope_view(views[1], x2, x2 if out2 is None else out2, n, rope.rot_dim, dev)
-    _on_device(dev, lambda s: lib().splash_rope(views, 1 if x2 is None else 2, _ptr(pos), pos.stride(0), n,
-                                                ctypes.byref(rope), s), stream)
+        _rope_view(views[1], x2, x2 if out2 is None else out2, n, rot, dev)
+    _on_device(dev, lib().splash_rope, (views, 1 if x2 is None else 2, positions.data_ptr(), strides[0] if axes > 1 else n,
+                                        n, rope), stream)
 
 
-def _gqa_cache(desc: GqaDesc, k_pages, v_pages, k_scales, v_scales):
+def _gqa_cache_ok(desc: GqaDesc, dev: int, k_pages, v_pages, k_scales, v_scales) -> bool:
+    scales, code = (desc.num_pages, desc.num_kv_heads), k_pages.dtype
+    pool = scales + (64, desc.head_dim)
+    return (k_pages.shape == pool and v_pages.shape == pool and k_scales.shape == scales and v_scales.shape == scales
+            and code is v_pages.dtype and code in _code_types(desc) and k_scales.dtype is _F32T and v_scales.dtype is _F32T
+            and k_pages.is_contiguous() and v_pages.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()
+            and 0 <= dev == k_pages.get_device() == v_pages.get_device() == k_scales.get_device() == v_scales.get_device())
+
+
+def _code_types(desc: GqaDesc):
     import torch
-    codes = (torch.uint8, torch.float8_e4m3fn) if desc.code_type == GQA_E4M3 else (torch.int8,)
-    pool = (desc.num_pages, desc.num_kv_heads, 64, desc.head_dim)
-    f32 = (torch.float32,)
-    return dict(k_pages=(k_pages, codes, pool), v_pages=(v_pages, codes, pool), k_scales=(k_scales, f32, pool[:2]),
-                v_scales=(v_scales, f32, pool[:2]))
+    return (torch.uint8, torch.float8_e4m3fn) if desc.code_type == GQA_E4M3 else (torch.int8,)
+
+
+def _refuse_gqa(desc: GqaDesc, dev: int, k_pages, v_pages, k_scales, v_scales, **tensors):
+    scales, codes = (desc.num_pages, desc.num_kv_heads), _code_types(desc)
+    pool = scales + (64, desc.head_dim)
+    _refuse_tensors(dev, k_pages=(k_pages, codes, pool), v_pages=(v_pages, codes, pool),
+                    k_scales=(k_scales, (_F32T,), scales), v_scales=(v_scales, (_F32T,), scales), **tensors)
 
 
 def splash_gqa_append(k_new, v_new, slots, k_pages, v_pages, k_scales, v_scales, desc: GqaDesc, stream=None) -> None:
     """Row t of k_new and v_new [rows, kv heads, head_dim] (views of one token and head stride) to slot slots[t]."""
-    import torch
-    n = slots.numel()
-    dev = _device_of(slots, slots=(slots, (torch.int32,), (n,)), **_gqa_cache(desc, k_pages, v_pages, k_scales, v_scales))
-    shape = (n, desc.num_kv_heads, desc.head_dim)
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or t.get_device() != dev:
-            _refuse(f"{name} must be bf16 {shape} on the cache's device")
-    if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
-        _refuse("k_new and v_new must have the same strides, the last dimension dense")
-    _on_device(dev, lambda s: lib().splash_gqa_append(
-        _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(slots), n, _ptr(k_pages), _ptr(v_pages),
-        _ptr(k_scales), _ptr(v_scales), ctypes.byref(desc), s), stream)
+    if _device is None:
+        _types()
+    n, dev = slots.numel(), slots.get_device()
+    shape, strides = (n, desc.num_kv_heads, desc.head_dim), k_new.stride()
+    if not (_gqa_cache_ok(desc, dev, k_pages, v_pages, k_scales, v_scales)
+            and slots.dtype is _I32T and slots.is_contiguous() and k_new.dtype is _BF16T and v_new.dtype is _BF16T
+            and k_new.shape == shape and v_new.shape == shape and dev == k_new.get_device() == v_new.get_device()
+            and strides == v_new.stride() and strides[2] == 1):
+        if k_new.shape == shape and v_new.shape == shape and (strides != v_new.stride() or strides[2] != 1):
+            _refuse("k_new and v_new must have the same strides, the last dimension dense")
+        bf16 = (_BF16T,)
+        _refuse_gqa(desc, dev, k_pages, v_pages, k_scales, v_scales, slots=(slots, (_I32T,), (n,)),
+                    k_new=(k_new.contiguous(), bf16, shape), v_new=(v_new.contiguous(), bf16, shape))
+    _on_device(dev, lib().splash_gqa_append, (
+        k_new.data_ptr(), v_new.data_ptr(), strides[0], strides[1], slots.data_ptr(), n, k_pages.data_ptr(),
+        v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), desc), stream)
 
 
 def splash_gqa_attend(q, k_pages, v_pages, k_scales, v_scales, block_table, seq_lens, q_chunk: int, out, lse,
                       desc: GqaDesc, workspace, stream=None) -> None:
-    import torch
-    rows = (desc.batch * q_chunk, desc.num_heads, desc.head_dim)
-    bf16, i32 = (torch.bfloat16,), (torch.int32,)
-    dev = _device_of(q, q=(q, bf16, rows), out=(out, bf16, rows), lse=(lse, (torch.float32,), rows[:2]),
-                     block_table=(block_table, i32, (desc.batch, desc.max_pages_per_seq)),
-                     seq_lens=(seq_lens, i32, (desc.batch,)), workspace=(workspace, (torch.uint8,), None),
-                     **_gqa_cache(desc, k_pages, v_pages, k_scales, v_scales))
-    _on_device(dev, lambda s: lib().splash_gqa_attend(
-        _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scales), _ptr(v_scales), _ptr(block_table), _ptr(seq_lens), q_chunk,
-        _ptr(out), _ptr(lse), ctypes.byref(desc), _ptr(workspace), workspace.numel(), s), stream)
+    """lse may be None."""
+    if _device is None:
+        _types()
+    dev, b, heads = q.get_device(), desc.batch, desc.num_heads
+    rows, table = (b * q_chunk, heads, desc.head_dim), (b, desc.max_pages_per_seq)
+    if not (_gqa_cache_ok(desc, dev, k_pages, v_pages, k_scales, v_scales)
+            and q.dtype is _BF16T and out.dtype is _BF16T and q.shape == rows and out.shape == rows
+            and block_table.dtype is _I32T and block_table.shape == table and seq_lens.dtype is _I32T
+            and seq_lens.numel() == b and workspace.element_size() == 1
+            and (lse is None or (lse.dtype is _F32T and lse.shape == rows[:2] and lse.is_contiguous() and lse.get_device() == dev))
+            and q.is_contiguous() and out.is_contiguous() and block_table.is_contiguous() and seq_lens.is_contiguous()
+            and workspace.is_contiguous() and dev == out.get_device() == block_table.get_device() == seq_lens.get_device()
+            == workspace.get_device()):
+        import torch
+        bf16, i32 = (_BF16T,), (_I32T,)
+        _refuse_gqa(desc, dev, k_pages, v_pages, k_scales, v_scales, q=(q, bf16, rows), out=(out, bf16, rows),
+                    lse=(lse, (_F32T,), rows[:2]), block_table=(block_table, i32, table), seq_lens=(seq_lens, i32, (b,)),
+                    workspace=(workspace, (torch.uint8, torch.int8), None))
+    _on_device(dev, lib().splash_gqa_attend, (
+        q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+        block_table.data_ptr(), seq_lens.data_ptr(), q_chunk, out.data_ptr(), None if lse is None else lse.data_ptr(), desc,
+        workspace.data_ptr(), workspace.numel()), stream)
 
 
 def version() -> str:
