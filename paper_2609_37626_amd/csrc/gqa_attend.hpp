@@ -253,8 +253,12 @@ __device__ __forceinline__ bool next_piece(const GqaAttendLaunch& a, int row_blo
     const int seq = history(a, w.b), pages = pages_of(seq), cost = pages + kTileCost;
     const int tile = __builtin_amdgcn_readfirstlane((w.at - w.b_start) / cost), start = w.b_start + tile * cost;
     const int hk = __builtin_amdgcn_readfirstlane(tile / row_blocks), rb = tile - hk * row_blocks;
-    const int p0 = max(w.at - start - kTileCost, 0), p1 = max(min(w.hi - start - kTileCost, pages), 0);
     const bool begins = w.at == start;
+    int p0 = max(w.at - start - kTileCost, 0), p1 = max(min(w.hi - start - kTileCost, pages), 0);
+    if (a.whole_tiles) {
+      p0 = begins ? 0 : pages;
+      p1 = pages;
+    }
     const Piece piece = {w.b, hk, rb * rows_per_tile, seq, p0, p1, p0 > 0 ? 2 * (int)blockIdx.x : p1 < pages ? 2 * (int)blockIdx.x + 1 : -1};
     w.at = start + cost;
     if (tile == tiles - 1) {
@@ -621,34 +625,49 @@ __global__ __launch_bounds__(64 * kWaves) void gqa_join_kernel(GqaAttendLaunch a
   const int r = tile.z * ROWS + rr;
   if (r >= a.q_chunk * a.group) return;
   const int parts = tile.w;
-  const auto slot = [&](int p) { return (int64_t)(p == 0 ? 2 * w + 1 : 2 * (w + p)); };
+  const auto at = [&](int p) { return (int64_t)(p == 0 ? 2 * w + 1 : 2 * (w + p)) * ROWS + rr; };
   const f32x2* ml = (const f32x2*)a.part_ml;
-  float top = kNegInf;
-  for (int p = lane; p < parts; p += 64) top = fmaxf(top, ml[slot(p) * ROWS + rr][0]);
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   constexpr int kLanes = D / 4, kSide = 64 / kLanes;  // lanes of a row; parts side by side
-  const int d = 4 * (lane % kLanes);
+  constexpr int kAhead = 8;                           // their loads, on the way before the weights are known
+  const int side = lane / kLanes, d = 4 * (lane % kLanes);
+  f32x4 x[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int p = side + k * kSide;
+    x[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    if (p < parts) x[k] = *(const f32x4*)(a.part_out + at(p) * D + d);
+  }
+  const f32x2 own = lane < parts ? ml[at(lane)] : (f32x2){kNegInf, 0.f};
+  float top = own[0];
+  for (int p = lane + 64; p < parts; p += 64) top = fmaxf(top, ml[at(p)][0]);
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) top = fmaxf(top, __shfl_xor(top, k));
+  const auto weight = [&](float m) { return m == kNegInf ? 0.f : __builtin_amdgcn_exp2f(m - top); };
+  const float by = weight(own[0]);
+  float sum = own[1] * by;
+  for (int p = lane + 64; p < parts; p += 64) {
+    const f32x2 v = ml[at(p)];
+    sum += v[1] * weight(v[0]);
+  }
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
-#pragma unroll 4
-  for (int p = lane / kLanes; p < parts; p += kSide) {
-    const int64_t at = slot(p) * ROWS + rr;
-    const f32x2 v = ml[at];
-    const f32x4 x = *(const f32x4*)(a.part_out + at * D + d);
-    if (v[0] != kNegInf) {
-      const float by = __builtin_amdgcn_exp2f(v[0] - top);
-      sum += v[1] * by;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(x[i], by, o[i]);
-    }
+  for (int k = 0; k < kAhead; ++k) {
+    const float f = __shfl(by, side + k * kSide);  // (0 past the last part: x is 0 there)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(x[k][i], f, o[i]);
+  }
+  for (int p = side + kAhead * kSide; p < parts; p += kSide) {
+    const float f = weight(ml[at(p)][0]);
+    const f32x4 y = *(const f32x4*)(a.part_out + at(p) * D + d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(y[i], f, o[i]);
   }
 #pragma unroll
-  for (int x = kLanes; x < 64; x <<= 1) {
-    sum += __shfl_xor(sum, x);
+  for (int k = kLanes; k < 64; k <<= 1)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], x);
-  }
+    for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], k);
   const int i = r / a.group, h = tile.y * a.group + r - i * a.group;
   const int64_t row = ((int64_t)tile.x * a.q_chunk + i) * (a.Hk * a.group) + h;
   if (lane < kLanes) {
@@ -666,9 +685,13 @@ hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
   // no more workgroups than the longest histories would fill
   const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * (a.bt_stride + kTileCost) + kLeastSpan - 1) / kLeastSpan;
   if (a.workers > most) a.workers = (int32_t)most;
+  // Few short tiles are not cut: each goes to the span that it begins in, and
+  // there is nothing to join (8 tiles of 2 to 8 pages: one launch of 8 us instead
+  // of 7 and 4). At 16 pages a wave has four.
+  a.whole_tiles = a.bt_stride <= 16 && (int64_t)a.B * a.Hk * row_blocks <= a.workers;
   hipLaunchKernelGGL((gqa_attend_kernel<D, MT, RG, CODE>), dim3(a.workers), dim3(64 * kWaves), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.whole_tiles) return e;
   hipLaunchKernelGGL((gqa_join_kernel<D, S::kRows>), dim3(a.workers, S::kRows / kWaves), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }

@@ -69,6 +69,7 @@ struct GqaAttendLaunch {
   float* lse;
   int32_t B, Hk, group, D, q_chunk, bt_stride, num_pages, code_type;
   float scale_log2;  // softmax_scale * log2(e)
+  bool whole_tiles;  // no tile is cut between workgroups
   int32_t workers;   // compute units; the launch makes it workgroups, at most kGqaMaxWorkers
   // workspace: two partial results per workgroup, of gqa_tile_rows() rows,
   // and {request, KV head, row block, parts} of the tile it begins (request -1: none)
