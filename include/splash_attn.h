@@ -402,7 +402,7 @@ typedef struct splash_gqa_desc {
     int32_t num_kv_heads;       /* 1 .. 128 */
     int32_t head_dim;           /* 64, 128 or 256 */
     int32_t page_size;          /* must be 64 */
-    int32_t max_pages_per_seq;  /* row stride of block_table, at least 1 */
+    int32_t max_pages_per_seq;  /* row stride of block_table, 1 .. 2^25 - 1 */
     int32_t num_pages;          /* pages in the pool, 1 .. 2^25 */
     int32_t code_type;          /* SPLASH_GQA_* */
     float softmax_scale;        /* multiplies <q, k>; finite and > 0 */
@@ -435,7 +435,7 @@ typedef struct splash_gqa_desc {
  *   requests     int32 [max_tokens]: the row's request (-1 on the rows behind)
  * Rows past max_tokens are not written; new_indptr counts them.  One launch.
  * Errors: INVALID_ARGUMENT (NULL buffer, batch or max_tokens or num_free < 0,
- * q_chunk < 0, max_pages_per_seq < 1, num_pages < 1, taken_out == taken_in),
+ * q_chunk < 0, max_pages_per_seq < 1, num_pages < 1, taken_out over taken_in),
  * MISALIGNED (a buffer not 4-byte aligned), UNSUPPORTED (batch > 8192,
  * num_pages > 2^25, 64 * max_pages_per_seq * batch past 2^31 - 1).
  */
@@ -459,12 +459,13 @@ int splash_step_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t
  *          the two must not overlap.  Only rot_dim elements of a head are read
  *          and written.
  *   positions  int32, axis a's position of token n at [a * position_stride + n];
- *          position_stride >= num_tokens where num_axes > 1
+ *          where num_axes > 1, position_stride >= num_tokens, or 0 (text: every
+ *          axis has the same positions)
  * inv_freq and pair_axis are HOST arrays of rot_dim / 2, read during the call.
  * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, num_axes outside
  * 1 .. 4, an axis outside [0, num_axes), an inv_freq or scale that is not
  * finite), UNSUPPORTED (rot_dim odd or outside 2 .. 256, more than 65536
- * heads), MISALIGNED (x or y not 2-byte, positions not 4-byte aligned).
+ * heads or 2^30 tokens), MISALIGNED (x or y not 2-byte, positions not 4-byte aligned).
  */
 typedef struct splash_rope_view {
     const void* x;
@@ -527,12 +528,14 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
  *   seq_lens   int32 [B], history lengths including the chunk
  *   out        bf16 [B*q_chunk, num_heads, head_dim] (round to nearest even)
  *   lse        fp32 [B*q_chunk, num_heads]; may be NULL
- *   workspace  splash_gqa_workspace_size(desc, q_chunk) bytes, 16-byte aligned
+ *   workspace  splash_gqa_workspace_size(desc, q_chunk) bytes, 16-byte aligned;
+ *              what it holds is of one call, and calls that may overlap (other
+ *              streams, graphs replayed side by side) take one each
  * Codes are converted exactly (K to bf16, V to fp16), products are summed in
  * fp32; a weight is rounded to fp16 before it meets V, and its sum is not.
  * Codes of places that no row of the request sees are not used, NaN codes
  * among them, and a place that some rows of a chunk do not see does not touch
- * those rows.  Deterministic: the same inputs give the same bits, wherever the
+ * those rows; NaN reaches the rows that see it (out and lse).  Deterministic: the same inputs give the same bits, wherever the
  * pages lie.
  * Errors: INVALID_ARGUMENT (desc, NULL, q_chunk < 1), UNSUPPORTED (desc;
  * a batch whose pages times heads pass 2^30), MISALIGNED (q, out, pages or

@@ -496,7 +496,7 @@ def _rope_view(view: RopeView, x, y, tokens: int, rot_dim: int, dev: int) -> Non
 
 def splash_rope(x, positions, rope: RopeDesc, out=None, x2=None, out2=None, stream=None) -> None:
     """Turns x (and x2) [tokens, heads, rot_dim], views of any token and head stride, by positions [tokens] or
-    [axes, tokens] into out (None: in place)."""
+    [axes, tokens] (or [tokens] expanded to it) into out (None: in place)."""
     if _device is None:
         _types()
     shape, strides, dev = positions.shape, positions.stride(), positions.get_device()

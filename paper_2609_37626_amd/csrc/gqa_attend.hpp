@@ -4,7 +4,7 @@
 // A tile is one request, one KV head and 16 to 128 of its query rows (q_chunk
 // rows times the heads that share the KV head): every K and V byte is read once
 // for all of them.  The tiles' pages, one tile after the other with
-// kTileCost places in front of each for its fixed work, form one line, which is
+// kGqaTileCost places in front of each for its fixed work, form one line, which is
 // cut into equal spans, one for each workgroup: long and short histories load
 // the chip alike without a plan, and only the tiles that a cut goes through
 // leave partial results, at most two a workgroup, which a second kernel joins.
@@ -46,10 +46,10 @@ constexpr float kWeightShift = 6.f;   // weights are 2^(z - m + 6)
 constexpr float kMoveAt = 8.f;        // the reference moves once a score passes it by this
 constexpr float kNegInf = -__builtin_inff();
 
-// Places of a tile in the line: kTileCost for its fixed work, then its pages.
-// A span is at least kLeastSpan places long: a page and a tile's fixed work
-// for each wave.
-constexpr int kTileCost = 8;
+// Places of a tile in the line: kGqaTileCost for its fixed work (two to three
+// steps' time: first loads, queries, the join; a ragged batch of 64 took 104 us
+// with 2, 90 with 4, 74 with 6, 68 with 8, 65 with 12, where 256 short ones lost
+// 1%), then its pages.  A span is at least kLeastSpan places long.
 constexpr int kLeastSpan = 6;
 
 // ---- codes to MFMA operands (exact) --------------------------------------
@@ -209,7 +209,7 @@ __device__ __forceinline__ Walk find_span(const GqaAttendLaunch& a, int tiles, i
   int mine = 0;
   for (int k = 0; k < per; ++k) {
     const int b = t * per + k;
-    if (b < a.B) mine += tiles * (pages_of(history(a, b)) + kTileCost);
+    if (b < a.B) mine += tiles * (pages_of(history(a, b)) + kGqaTileCost);
   }
   int upto = mine;
 #pragma unroll
@@ -229,7 +229,7 @@ __device__ __forceinline__ Walk find_span(const GqaAttendLaunch& a, int tiles, i
   if (lo < hi && lo >= upto - mine && lo < upto) {
     int start = upto - mine;
     for (int b = t * per;; ++b) {
-      const int next = start + tiles * (pages_of(history(a, b)) + kTileCost);
+      const int next = start + tiles * (pages_of(history(a, b)) + kGqaTileCost);
       if (lo < next) {
         lds[kWaves] = b;
         lds[kWaves + 1] = start;
@@ -250,11 +250,11 @@ __device__ __forceinline__ Walk find_span(const GqaAttendLaunch& a, int tiles, i
 __device__ __forceinline__ bool next_piece(const GqaAttendLaunch& a, int row_blocks, int rows_per_tile, Walk& w, Piece* out) {
   const int tiles = a.Hk * row_blocks;
   while (w.at < w.hi) {
-    const int seq = history(a, w.b), pages = pages_of(seq), cost = pages + kTileCost;
+    const int seq = history(a, w.b), pages = pages_of(seq), cost = pages + kGqaTileCost;
     const int tile = __builtin_amdgcn_readfirstlane((w.at - w.b_start) / cost), start = w.b_start + tile * cost;
     const int hk = __builtin_amdgcn_readfirstlane(tile / row_blocks), rb = tile - hk * row_blocks;
     const bool begins = w.at == start;
-    int p0 = max(w.at - start - kTileCost, 0), p1 = max(min(w.hi - start - kTileCost, pages), 0);
+    int p0 = max(w.at - start - kGqaTileCost, 0), p1 = max(min(w.hi - start - kGqaTileCost, pages), 0);
     if (a.whole_tiles) {
       p0 = begins ? 0 : pages;
       p1 = pages;
@@ -268,7 +268,7 @@ __device__ __forceinline__ bool next_piece(const GqaAttendLaunch& a, int row_blo
     // (a tile without a page belongs to the span of its first place)
     if (p0 < p1 || (pages == 0 && begins)) {
       if (p0 == 0 && p1 < pages)
-        w.joined = {piece.b, hk, rb, (start + kTileCost + pages - 1) / w.chunk - (int)blockIdx.x + 1};
+        w.joined = {piece.b, hk, rb, (start + kGqaTileCost + pages - 1) / w.chunk - (int)blockIdx.x + 1};
       *out = piece;
       return true;
     }
@@ -308,7 +308,7 @@ __device__ __forceinline__ void join_waves(const GqaAttendLaunch& a, const Piece
     for (int w = 0; w < S::kLanes; ++w) {
       const int at = (first + w) * S::kWaveRows + 16 * mt + c;
       const float mw = lds_m[at];
-      sum += mw == kNegInf ? 0.f : lds_l[at] * __builtin_amdgcn_exp2f(mw - top);
+      sum += mw == kNegInf ? lds_l[at] : lds_l[at] * __builtin_amdgcn_exp2f(mw - top);  // (0 there, or NaN)
     }
     const int rr = wave / S::kLanes * S::kWaveRows + 16 * mt + c, r = t.row0 + rr;
     if (slot >= 0) {
@@ -683,7 +683,7 @@ hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
   const int64_t row_blocks = ((int64_t)a.q_chunk * a.group + S::kRows - 1) / S::kRows;
   a.workers = a.workers * S::kPerCu < kGqaMaxWorkers ? a.workers * S::kPerCu : kGqaMaxWorkers;
   // no more workgroups than the longest histories would fill
-  const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * (a.bt_stride + kTileCost) + kLeastSpan - 1) / kLeastSpan;
+  const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * (a.bt_stride + kGqaTileCost) + kLeastSpan - 1) / kLeastSpan;
   if (a.workers > most) a.workers = (int32_t)most;
   // Few short tiles are not cut: each goes to the span that it begins in, and
   // there is nothing to join (8 tiles of 2 to 8 pages: one launch of 8 us instead

@@ -36,6 +36,8 @@ int validate_gqa(const splash_gqa_desc* d) {
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "max_pages_per_seq and num_pages must be >= 1");
   if (d->num_pages > kMaxPoolPages)
     return fail(SPLASH_ERR_UNSUPPORTED, "num_pages must be at most 2^25 (got %d)", d->num_pages);
+  if (d->max_pages_per_seq > INT32_MAX / kPage)  // (positions are int32)
+    return fail(SPLASH_ERR_UNSUPPORTED, "max_pages_per_seq must be at most 2^25 - 1 (got %d)", d->max_pages_per_seq);
   if (!(std::isfinite(d->softmax_scale) && d->softmax_scale > 0.f))
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
   return SPLASH_OK;
@@ -84,10 +86,12 @@ int splash_step_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t
   if (!taken_in || !taken_out || !new_indptr || (batch > 0 && (!seq_lens || !block_table)) ||
       (num_free > 0 && !free_pages) || (max_tokens > 0 && (!slots || !positions || !requests)))
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "NULL buffer");
-  if (taken_in == taken_out) return fail(SPLASH_ERR_INVALID_ARGUMENT, "taken_out must not be taken_in");
   const void* ints[] = {seq_lens, new_lens, free_pages, taken_in, taken_out, block_table, new_indptr, slots, positions, requests};
   for (const void* p : ints)
     if (!aligned(p, 4)) return fail(SPLASH_ERR_MISALIGNED, "int32 buffers must be 4-byte aligned");
+  const uintptr_t in = reinterpret_cast<uintptr_t>(taken_in), out = reinterpret_cast<uintptr_t>(taken_out);
+  if ((in < out ? out - in : in - out) < 2 * sizeof(int32_t))
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "taken_out must not overlap taken_in");
   const TablesLaunch t = {seq_lens,  new_lens,    q_chunk,           batch,     free_pages, num_free,   taken_in,  taken_out,
                           block_table, max_pages_per_seq, num_pages, max_tokens, new_indptr, slots,     positions, requests};
   const hipError_t e = launch_step_tables(t, static_cast<hipStream_t>(stream));
@@ -99,6 +103,7 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
   if (!views || !desc || !desc->inv_freq) return fail(SPLASH_ERR_INVALID_ARGUMENT, "views, desc and inv_freq must be non-NULL");
   if (num_views < 1 || num_views > 2) return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_views must be 1 or 2 (got %d)", num_views);
   if (num_tokens < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_tokens < 0");
+  if (num_tokens > 1 << 30) return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens must be at most 2^30 (got %d)", num_tokens);
   if (desc->rot_dim < 2 || desc->rot_dim > 2 * kMaxRopePairs || desc->rot_dim % 2)
     return fail(SPLASH_ERR_UNSUPPORTED, "rot_dim must be even, 2 .. %d (got %d)", 2 * kMaxRopePairs, desc->rot_dim);
   if (desc->num_axes < 1 || desc->num_axes > 4)
@@ -139,8 +144,8 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
   if (num_tokens == 0) return SPLASH_OK;
   if (!positions) return fail(SPLASH_ERR_INVALID_ARGUMENT, "positions is NULL");
   if (!aligned(positions, 4)) return fail(SPLASH_ERR_MISALIGNED, "positions not 4-byte aligned");
-  if (desc->num_axes > 1 && position_stride < num_tokens)
-    return fail(SPLASH_ERR_INVALID_ARGUMENT, "position_stride must be at least num_tokens");
+  if (desc->num_axes > 1 && position_stride < num_tokens && position_stride != 0)
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "position_stride must be 0 or at least num_tokens");
   const hipError_t e = launch_rope(r, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SPLASH_OK : hip_fail(e, "rope launch");
 }
@@ -195,7 +200,7 @@ int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, c
   // and per-tile shares that their positions count stay below 2^30
   const int64_t row_blocks = ((int64_t)q_chunk * group + 15) / 16;
   const int64_t tiles = row_blocks > (1 << 20) ? INT64_MAX : (int64_t)desc->batch * desc->num_kv_heads * row_blocks;
-  if (tiles > (1 << 30) || tiles * ((int64_t)desc->max_pages_per_seq + 8) > (1 << 30))
+  if (tiles > (1 << 30) || tiles * ((int64_t)desc->max_pages_per_seq + kGqaTileCost) > (1 << 30))
     return fail(SPLASH_ERR_UNSUPPORTED, "batch * num_kv_heads * row blocks * pages passes 2^30");
   const GqaLayout layout = gqa_layout(desc, q_chunk);
   if (ws_bytes < layout.total)

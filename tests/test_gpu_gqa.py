@@ -76,6 +76,36 @@ def test_attend_nan_codes_stay_with_the_rows_that_see_them():
     assert np.array_equal(nan, want) and bool(torch.isfinite(lse).all())
 
 
+@pytest.mark.parametrize("lens", [[200, 64, 130], [9000, 64, 130]], ids=["whole", "split"])
+def test_attend_nan_and_infinite_queries_stay_in_their_rows(lens):
+    p = Attend(lens, 2, 4, 64, 2, False, seed=11)
+    ref = p.oracle()
+    p.q[1, 3, 7] = 0x7FC0
+    p.q[4, 6, 0] = 0x7F80
+    out, lse = p.attend()
+    o, l = out.float().cpu().numpy(), lse.cpu().numpy()
+    for row, head in ((1, 3), (4, 6)):
+        assert np.isnan(o[row, head]).all() and np.isnan(l[row, head])
+        o[row, head], l[row, head] = ref[0][row, head], ref[1][row, head]
+    np.testing.assert_allclose(o, ref[0], atol=2e-2)
+    np.testing.assert_allclose(l, ref[1], atol=1e-4)
+
+
+def test_attend_calls_side_by_side_on_two_streams():
+    ps = [Attend([5000, 70], 2, 8, 128, 1, False, seed=26), Attend([3000, 1, 900], 1, 16, 64, 2, True, seed=27)]
+    want = [p.attend() for p in ps]
+    streams = [torch.cuda.Stream() for _ in ps]
+    state = [(p.device(), p.workspace(), p.outputs()) for p in ps]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, s, (t, ws, (out, lse)) in zip(ps, streams, state):
+            B.splash_gqa_attend(t["q"], t["k_pages"], t["v_pages"], t["k_scales"], t["v_scales"], t["block_table"],
+                                t["seq_lens"], p.q_chunk, out, lse, p.desc(), ws, stream=s)
+    torch.cuda.synchronize()
+    for (a, la), (_, _, (b, lb)) in zip(want, state):
+        assert torch.equal(a, b) and torch.equal(la, lb)
+
+
 def test_attend_skips_pages_outside_the_pool():
     p = Attend([300, 500, 60], 2, 4, 64, 2, True, seed=12)
     p.table[0, 1], p.table[1, 7], p.table[2, 0] = -1, p.k.shape[0], 1 << 30

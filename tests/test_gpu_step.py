@@ -160,6 +160,16 @@ def test_rope_views_leave_the_rest_of_a_row(interleaved, head, offset, rot):
     check_rope(bf16_bits(before[:, 1:5, offset:offset + rot]), bf16_bits(turned), pos, freq, axis, interleaved, 1.25)
 
 
+def test_rope_of_text_positions_on_every_axis():
+    rng = np.random.Generator(np.random.PCG64(41))
+    x = bf16(rng, 50, 3, 64)
+    freq, axis = 0.8 ** np.arange(32), np.arange(32) % 3
+    pos = rng.integers(0, 9000, 50).astype(np.int32)
+    out = to_bf16(x)
+    B.splash_rope(out, dev(pos).expand(3, -1), B.make_rope(64, freq, pair_axis=axis))
+    check_rope(x, bf16_bits(out), np.broadcast_to(pos, (3, 50)), freq, axis, False)
+
+
 def test_rope_refuses_other_shapes():
     x, rope = torch.zeros((3, 2, 8), dtype=torch.bfloat16, device="cuda"), B.make_rope(8, [1.0] * 4)
     pos = torch.zeros(3, dtype=torch.int32, device="cuda")

@@ -1,9 +1,11 @@
 """Refusals of the serving-step calls, before any launch (no GPU): the C entry
 points on addresses that are never read, and the binding's tensor checks."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import numpy as np
-import os
 import pytest
 import torch
 
@@ -11,6 +13,7 @@ from paper_2609_37626_amd import binding as B
 
 pytestmark = pytest.mark.skipif(not os.path.exists(B.LIB_PATH), reason="library not built")
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 1 << 20
 BAD, UNSUPPORTED, MISALIGNED, SMALL = (B.SPLASH_ERR_INVALID_ARGUMENT, B.SPLASH_ERR_UNSUPPORTED, B.SPLASH_ERR_MISALIGNED,
                                        B.SPLASH_ERR_WORKSPACE_TOO_SMALL)
@@ -39,7 +42,7 @@ def append(d, k=FAKE, v=FAKE, ts=128, hs=64, slots=FAKE, n=4, kp=FAKE, vp=FAKE, 
     (dict(page_size=16), UNSUPPORTED), (dict(head_dim=96), UNSUPPORTED), (dict(num_heads=15), UNSUPPORTED),
     (dict(num_heads=0), UNSUPPORTED), (dict(num_kv_heads=0), UNSUPPORTED), (dict(num_heads=2048), UNSUPPORTED),
     (dict(num_heads=258, num_kv_heads=129), UNSUPPORTED), (dict(code_type=2), UNSUPPORTED),
-    (dict(num_pages=(1 << 25) + 1), UNSUPPORTED),
+    (dict(num_pages=(1 << 25) + 1), UNSUPPORTED), (dict(max_pages_per_seq=1 << 25), UNSUPPORTED),
 ])
 def test_bad_gqa_descriptor(mutate, status):
     assert attend(desc(**mutate)) == status
@@ -94,6 +97,7 @@ def test_step_tables_arguments():
         assert tables(**{name: None}) == BAD, name
         assert tables(**{name: FAKE + 66}) == MISALIGNED, name
     assert tables(new=FAKE + 2) == MISALIGNED
+    assert tables(taken_out=FAKE + 4) == BAD and tables(taken=FAKE + 4, taken_out=FAKE) == BAD   # overlap
     assert tables(batch=8193) == UNSUPPORTED and tables(pages=(1 << 25) + 1) == UNSUPPORTED
     assert tables(batch=8192, width=1 << 13) == UNSUPPORTED
 
@@ -112,7 +116,7 @@ def test_rope_arguments():
     assert rope(views=0) == BAD and rope(views=3) == BAD and rope(n=-1) == BAD and rope(heads=-1) == BAD
     assert rope(axes=0) == BAD and rope(axes=5) == BAD and rope(scale=float("nan")) == BAD
     assert rope(rot=63) == UNSUPPORTED and rope(rot=0) == UNSUPPORTED and rope(rot=258) == UNSUPPORTED
-    assert rope(heads=65537) == UNSUPPORTED
+    assert rope(heads=65537) == UNSUPPORTED and rope(n=(1 << 30) + 1) == UNSUPPORTED
     assert rope(freq=[1.0] * 31 + [float("inf")]) == BAD
     assert rope(axis=[0] * 31 + [1]) == BAD and rope(axes=2, axis=[0] * 31 + [2]) == BAD
     assert rope(x=None) == BAD and rope(y=None) == BAD and rope(pos=None) == BAD
@@ -138,3 +142,22 @@ def test_binding_refuses_host_tensors_and_bad_descriptors():
         B.splash_rope(x, torch.zeros(2, dtype=torch.int32), B.make_rope(8, [1.0] * 4))
     with pytest.raises(B.SplashError):
         B.gqa_workspace_size(desc(head_dim=80), 1)
+
+
+def test_step_checks_under_host_sanitizers(tmp_path):
+    """The checks over random and extreme arguments, built with host sanitizers against stubs of the launchers."""
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("hipcc not found")
+    csrc, exe = os.path.join(ROOT, "paper_2609_37626_amd", "csrc"), tmp_path / "step_fuzz"
+    r = subprocess.run([hipcc, "--offload-arch=gfx950", "-O1", "-g", "-std=c++17",
+                        "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+                        "-Xarch_host", "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                        os.path.join(csrc, "api.cpp"), os.path.join(csrc, "step_api.cpp"),
+                        os.path.join(ROOT, "tests", "sanitize", "launch_stubs.cpp"),
+                        os.path.join(ROOT, "tests", "sanitize", "step_fuzz.cpp"), "-o", str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=1", UBSAN_OPTIONS="print_stacktrace=1")
+    r = subprocess.run([str(exe), "200000"], capture_output=True, text=True, env=env, timeout=300)
+    assert r.returncode == 0, r.stderr[-4000:]
+    assert r.stdout.startswith("ok ") and int(r.stdout.split()[1]) > 1000   # calls that reached a launch
