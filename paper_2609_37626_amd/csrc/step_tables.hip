@@ -20,7 +20,8 @@ namespace splash {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kRowsPerGroup = 4096;
+constexpr int kRowsPerGroup = kThreads;  // (131,072 rows: 5.4 us, with 4,096 rows a workgroup 8.8)
+constexpr int kPerThread = kMaxTableBatch / kThreads;
 
 struct Lens {
   int32_t seq, fresh;  // tokens after the step, and the new ones among them
@@ -40,15 +41,22 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(TablesLaunch p) {
   __shared__ int32_t wave_rows[kThreads / 64], wave_pages[kThreads / 64];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
 
+  // The thread's requests, all their lengths on the way at once.
   const int per = (p.B + kThreads - 1) / kThreads;
-  int32_t rows = 0, pages = 0;
-  for (int k = 0; k < per; ++k) {
-    const int b = t * per + k;
-    if (b < p.B) {
-      const Lens n = request_lens(p, b);
-      rows += n.fresh;
-      pages += pages_of(n.seq) - pages_of(n.seq - n.fresh);
+  int32_t fresh[kPerThread], need[kPerThread], rows = 0, pages = 0;
+#pragma unroll
+  for (int k = 0; k < kPerThread; ++k) {
+    fresh[k] = need[k] = 0;
+    if (k < per) {
+      const int b = t * per + k;
+      const Lens n = request_lens(p, min(b, p.B - 1));
+      if (b < p.B) {
+        fresh[k] = n.fresh;
+        need[k] = pages_of(n.seq) - pages_of(n.seq - n.fresh);
+      }
     }
+    rows += fresh[k];
+    pages += need[k];
   }
   int32_t rows_in = rows, pages_in = pages;  // inclusive over the wave, then the workgroup
 #pragma unroll
@@ -70,15 +78,15 @@ __global__ __launch_bounds__(kThreads) void step_tables_kernel(TablesLaunch p) {
   }
   rows_in -= rows;
   pages_in -= pages;
-  for (int k = 0; k < per; ++k) {
+#pragma unroll
+  for (int k = 0; k < kPerThread; ++k) {
     const int b = t * per + k;
-    if (b < p.B) {
-      const Lens n = request_lens(p, b);
+    if (k < per && b < p.B) {
       row_at[b] = rows_in;
       page_at[b] = pages_in;
-      rows_in += n.fresh;
-      pages_in += pages_of(n.seq) - pages_of(n.seq - n.fresh);
     }
+    rows_in += fresh[k];
+    pages_in += need[k];
   }
   if (t == kThreads - 1) {
     row_at[p.B] = rows_in;
