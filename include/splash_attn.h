@@ -505,6 +505,7 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
  *   new rows: code = x * 2^-e, rounded to nearest even; infinities take the
  *         largest code of their sign; NaN is E4M3's NaN and INT8's 0
  *   scale = 2^e
+ * desc->batch, the step's requests, decides only how the work is laid out.
  * A block that is continued must have a power-of-two scale (as this call
  * writes it; of another, its exponent alone is used).  Rows of a block past its
  * last new place are not written.

@@ -50,7 +50,7 @@ struct GqaAppendLaunch {
   const uint16_t* v_new;
   int64_t token_stride, head_stride;
   const int32_t* slots;
-  int32_t num_tokens, Hk, D, num_pages, code_type;
+  int32_t num_tokens, batch, Hk, D, num_pages, code_type;
   uint8_t* k_pages;
   uint8_t* v_pages;
   float* k_scales;

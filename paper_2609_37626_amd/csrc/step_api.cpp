@@ -164,7 +164,7 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
     return fail(SPLASH_ERR_MISALIGNED, "k_new and v_new must be 16-byte aligned, with strides of whole 8 elements");
   if (!aligned(slots, 4)) return fail(SPLASH_ERR_MISALIGNED, "slots not 4-byte aligned");
   const GqaAppendLaunch a = {static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), token_stride,
-                             head_stride, slots, num_tokens, desc->num_kv_heads, desc->head_dim, desc->num_pages,
+                             head_stride, slots, num_tokens, desc->batch, desc->num_kv_heads, desc->head_dim, desc->num_pages,
                              desc->code_type, static_cast<uint8_t*>(k_pages), static_cast<uint8_t*>(v_pages),
                              k_scales, v_scales};
   const hipError_t e = launch_gqa_append(a, static_cast<hipStream_t>(stream));

@@ -214,9 +214,9 @@ def test_attend_replays_in_a_graph():
 
 # -------------------------------------------------------------- append ---
 
-def run_append(k, v, slots, cache, scales, int8, heads, dim, strided=False):
+def run_append(k, v, slots, cache, scales, int8, heads, dim, strided=False, batch=1):
     pages = cache[0].shape[0]
-    desc = B.make_gqa_desc(1, heads, heads, dim, 1, pages, B.GQA_INT8 if int8 else B.GQA_E4M3)
+    desc = B.make_gqa_desc(batch, heads, heads, dim, 1, pages, B.GQA_INT8 if int8 else B.GQA_E4M3)
     dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()
     kt, vt = to_bf16(k), to_bf16(v)
     if strided:  # keys and values side by side in one row, behind the queries
@@ -232,12 +232,13 @@ def run_append(k, v, slots, cache, scales, int8, heads, dim, strided=False):
 def check_append(k, v, slots, int8, heads, dim, seed, pages=12, exponents=(-9, -5), strided=False):
     rng = np.random.Generator(np.random.PCG64(seed))
     cache, scales = zip(*[blocks(rng, pages, heads, dim, int8, exponents) for _ in range(2)])
-    got_c, got_s = run_append(k, v, slots, cache, scales, int8, heads, dim, strided)
-    for x, c, s, gc, gs in zip((k, v), cache, scales, got_c, got_s):
-        want_c, want_s = oracle.step.gqa_append(x, slots, c, s, int8)
-        assert np.array_equal(gs, want_s)
-        nan = (want_c & 0x7F) == 0x7F if not int8 else np.zeros(want_c.shape, bool)
-        assert np.array_equal(gc[~nan], want_c[~nan]) and np.all((gc[nan] & 0x7F) == 0x7F)
+    want = [oracle.step.gqa_append(x, slots, c, s, int8) for x, c, s in zip((k, v), cache, scales)]
+    for batch in (1, 1000):   # laid out for prompts (from 8 rows on), and for decode steps
+        got_c, got_s = run_append(k, v, slots, cache, scales, int8, heads, dim, strided, batch)
+        for (want_c, want_s), gc, gs in zip(want, got_c, got_s):
+            assert np.array_equal(gs, want_s)
+            nan = (want_c & 0x7F) == 0x7F if not int8 else np.zeros(want_c.shape, bool)
+            assert np.array_equal(gc[~nan], want_c[~nan]) and np.all((gc[nan] & 0x7F) == 0x7F)
 
 
 SLOTS = {
@@ -248,6 +249,10 @@ SLOTS = {
     "skips": [-1, 64 * 1 + 5, -1, 64 * 12, 64 * 4 + 1, 64 * 4 + 3, -(1 << 31), 2 ** 31 - 1],
     "backwards": [64 * 3 + r for r in (9, 4, 63, 2)],
     "page": list(range(64 * 8, 64 * 9)),
+    # short and long runs in one stretch of the list, over its 32- and 64-row ends
+    "mixed": sum(([64 * p + r for r in range(at, at + n)] for p, at, n in
+                  [(0, 5, 1), (1, 0, 8), (2, 55, 9), (3, 63, 1), (4, 0, 2), (5, 10, 40), (6, 1, 1), (7, 2, 7), (8, 0, 1), (9, 20, 3)]),
+                 []) + [64 * 10 + r for r in (7, 3, 30, 1, 2, 9, 8, 40, 50, 49)] + [64 * 11 + 62, 64 * 11 + 60],
 }
 
 
