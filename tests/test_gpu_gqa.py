@@ -41,6 +41,19 @@ def test_attend_long_and_ragged(int8, dim, group, q_chunk):
     check(Attend([20000, 17, 4097, 9000, 640], 1, group, dim, q_chunk, int8, seed=7).poison(), f"d{dim} g{group} q{q_chunk}")
 
 
+@pytest.mark.parametrize("int8", [False, True], ids=["e4m3", "int8"])
+@pytest.mark.parametrize("dim,kv_heads,group,q_chunk", [(64, 2, 4, 1), (128, 3, 2, 4), (128, 1, 16, 8), (256, 2, 16, 4)])
+def test_attend_edges_beside_a_long_history(int8, dim, kv_heads, group, q_chunk):
+    # (a table row past 16 pages: tiles are cut, short and empty ones among them)
+    check(Attend([0, 1, 1100, 63, 0, 64, 65, 2, 0], kv_heads, group, dim, q_chunk, int8, seed=28).poison())
+
+
+@pytest.mark.parametrize("dim,q_chunk,lens", [(128, 150, [150, 400, 149, 90]), (256, 70, [70, 1300]), (64, 200, [1500, 3])])
+def test_attend_long_chunks(dim, q_chunk, lens):
+    # a prompt's rows: several row blocks, most pages seen in part
+    check(Attend(lens, 1, 2, dim, q_chunk, False, seed=29).poison(), f"d{dim} q{q_chunk}")
+
+
 def test_attend_many_requests():
     rng = np.random.Generator(np.random.PCG64(5))
     check(Attend(rng.integers(0, 200, 700), 2, 4, 64, 1, False, seed=8).poison())
