@@ -456,7 +456,7 @@ int splash_step_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t
  *   view   x, y: bf16, element d of head h of token n at
  *          n * token_stride + h * head_stride + d (strides in elements, of x
  *          and y each); y == x with the same strides rotates in place, else
- *          the two must not overlap.  Only rot_dim elements of a head are read
+ *          the two must not overlap, and no y another view.  Only rot_dim elements of a head are read
  *          and written.
  *   positions  int32, axis a's position of token n at [a * position_stride + n];
  *          where num_axes > 1, position_stride >= num_tokens, or 0 (text: every
@@ -465,7 +465,7 @@ int splash_step_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t
  * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, num_axes outside
  * 1 .. 4, an axis outside [0, num_axes), an inv_freq or scale that is not
  * finite), UNSUPPORTED (rot_dim odd or outside 2 .. 256, more than 65536
- * heads or 2^30 tokens), MISALIGNED (x or y not 2-byte, positions not 4-byte aligned).
+ * heads or 2^25 tokens), MISALIGNED (x or y not 2-byte, positions not 4-byte aligned).
  */
 typedef struct splash_rope_view {
     const void* x;
@@ -510,7 +510,7 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
  * writes it; of another, its exponent alone is used).  Rows of a block past its
  * last new place are not written.
  * Errors: INVALID_ARGUMENT (desc, NULL, num_tokens < 0, negative stride),
- * UNSUPPORTED (desc), MISALIGNED (pages not 16-byte, scales or slots not 4-byte,
+ * UNSUPPORTED (desc, num_tokens * num_kv_heads past 2^25), MISALIGNED (pages not 16-byte, scales or slots not 4-byte,
  * k_new and v_new not 16-byte aligned, strides not multiples of 8 elements).
  */
 int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride, int64_t head_stride,
@@ -536,8 +536,9 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
  * fp32; a weight is rounded to fp16 before it meets V, and its sum is not.
  * Codes of places that no row of the request sees are not used, NaN codes
  * among them, and a place that some rows of a chunk do not see does not touch
- * those rows; NaN reaches the rows that see it (out and lse).  Deterministic: the same inputs give the same bits, wherever the
- * pages lie.
+ * those rows; NaN reaches the rows that see it (out and lse).  Values of V up
+ * to 2^80 cannot overflow the sums, whatever the lengths.  Deterministic: the
+ * same inputs give the same bits, wherever the pages lie.
  * Errors: INVALID_ARGUMENT (desc, NULL, q_chunk < 1), UNSUPPORTED (desc;
  * a batch whose pages times heads pass 2^30), MISALIGNED (q, out, pages or
  * workspace not 16-byte, other arrays not 4-byte aligned),

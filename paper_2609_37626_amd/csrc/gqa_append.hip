@@ -335,7 +335,6 @@ hipError_t launch_code(const GqaAppendLaunch& a, hipStream_t s) {
   const int64_t waves = prompts ? ((int64_t)a.num_tokens + kWindow - 1) / kWindow * 2 * a.Hk
                                 : (int64_t)a.num_tokens * ((2 * a.Hk + kGroups - 1) / kGroups);
   const int64_t groups = (waves + kThreads / 64 - 1) / (kThreads / 64);
-  if (groups > 0x7fffffff) return hipErrorInvalidConfiguration;
   if (prompts) hipLaunchKernelGGL((gqa_append_prompts_kernel<D, CODE>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
   else hipLaunchKernelGGL((gqa_append_rows_kernel<D, CODE>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
   return hipGetLastError();

@@ -87,6 +87,12 @@ __device__ __forceinline__ uint32_t pair_to_f16(uint32_t pair) {
   }
 }
 
+// What brings a K block's products to base-2 scores: kept off 0 and infinity, so
+// that masked products stay -inf and zeros stay 0 whatever the two scales are.
+__device__ __forceinline__ float score_scale(float k_scale, float scale_log2) {
+  return __builtin_amdgcn_fmed3f(k_scale * scale_log2, 0x1p-149f, 0x1.fffffep127f);
+}
+
 __device__ __forceinline__ float xor_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
@@ -451,7 +457,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
 #pragma unroll
       for (int j = 0; j < S::kDims; ++j) o[j][mt] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
-    float ks = scalar_load(a.k_scales + block) * a.scale_log2, vs = scalar_load(a.v_scales + block);
+    float ks = score_scale(scalar_load(a.k_scales + block), a.scale_log2), vs = scalar_load(a.v_scales + block);
     for (int n = 0; n < pages; ++n) {
       const int p = t.p0 + turn + n * S::kLanes;
       const bool held = (unsigned)page < (unsigned)a.num_pages;
@@ -460,7 +466,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
       const uint8_t* vb = a.v_pages + block * (kPage * D);
       const int after = n + 2 < pages ? entry(t, n + 2) : entry(next_t, n + 2 - pages);
       const int64_t next_block = block_of(next, n + 1 < pages ? t.hk : next_t.hk);
-      const float next_ks = scalar_load(a.k_scales + next_block) * a.scale_log2, next_vs = scalar_load(a.v_scales + next_block);
+      const float next_ks = score_scale(scalar_load(a.k_scales + next_block), a.scale_log2), next_vs = scalar_load(a.v_scales + next_block);
       load_v(block);
       __builtin_amdgcn_sched_barrier(0);
 

@@ -18,6 +18,9 @@ namespace {
 bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 constexpr int32_t kMaxPoolPages = 1 << 25;  // a slot (64 * page + place) fits int32
+// A launch holds less than 2^32 lanes: 64 a token, or a token and KV head.
+constexpr int32_t kMaxRopeTokens = 1 << 25;
+constexpr int64_t kMaxAppendRows = 1 << 25;
 
 int validate_gqa(const splash_gqa_desc* d) {
   if (!d) return fail(SPLASH_ERR_INVALID_ARGUMENT, "desc is NULL");
@@ -103,7 +106,7 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
   if (!views || !desc || !desc->inv_freq) return fail(SPLASH_ERR_INVALID_ARGUMENT, "views, desc and inv_freq must be non-NULL");
   if (num_views < 1 || num_views > 2) return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_views must be 1 or 2 (got %d)", num_views);
   if (num_tokens < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_tokens < 0");
-  if (num_tokens > 1 << 30) return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens must be at most 2^30 (got %d)", num_tokens);
+  if (num_tokens > kMaxRopeTokens) return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens must be at most 2^25 (got %d)", num_tokens);
   if (desc->rot_dim < 2 || desc->rot_dim > 2 * kMaxRopePairs || desc->rot_dim % 2)
     return fail(SPLASH_ERR_UNSUPPORTED, "rot_dim must be even, 2 .. %d (got %d)", 2 * kMaxRopePairs, desc->rot_dim);
   if (desc->num_axes < 1 || desc->num_axes > 4)
@@ -157,6 +160,8 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
   if (st != SPLASH_OK) return st;
   if (num_tokens < 0 || token_stride < 0 || head_stride < 0)
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_tokens and strides must be >= 0");
+  if ((int64_t)num_tokens * desc->num_kv_heads > kMaxAppendRows)
+    return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens * num_kv_heads passes 2^25");
   if (num_tokens == 0 || desc->batch == 0) return SPLASH_OK;
   if (!k_new || !v_new || !slots) return fail(SPLASH_ERR_INVALID_ARGUMENT, "k_new, v_new and slots must be non-NULL");
   if ((st = check_gqa_cache(k_pages, v_pages, k_scales, v_scales)) != SPLASH_OK) return st;

@@ -29,13 +29,13 @@ hipError_t launch_step_tables(const TablesLaunch& p, hipStream_t) {
 }
 hipError_t launch_rope(const RopeLaunch& p, hipStream_t) {
   ++launches;
-  need(p.pairs >= 1 && p.pairs <= kMaxRopePairs && p.num_tokens >= 1 && p.num_tokens <= 1 << 30, "rope");
+  need(p.pairs >= 1 && p.pairs <= kMaxRopePairs && p.num_tokens >= 1 && p.num_tokens <= 1 << 25, "rope");
   for (int j = 0; j < p.pairs; ++j) need(p.axis[j] < 4, "axis");
   return hipSuccess;
 }
 hipError_t launch_gqa_append(const GqaAppendLaunch& p, hipStream_t) {
   ++launches;
-  need(p.num_tokens >= 1 && p.num_pages <= 1 << 25 && p.Hk >= 1 && p.token_stride % 8 == 0, "append");
+  need(p.num_tokens >= 1 && (int64_t)p.num_tokens * p.Hk <= 1 << 25 && p.num_pages <= 1 << 25 && p.Hk >= 1 && p.token_stride % 8 == 0, "append");
   return hipSuccess;
 }
 hipError_t launch_gqa_attend(const GqaAttendLaunch& p, hipStream_t) {

@@ -67,6 +67,21 @@ def test_attend_scales_far_apart_and_sharp_scores(int8):
     check(Attend([1000, 300], 2, 4, 128, 2, int8, seed=10, q_scale=30.0))
 
 
+@pytest.mark.parametrize("softmax_scale", [2.0 ** -60, 2.0 ** 60])
+@pytest.mark.parametrize("lens", [[70, 200, 3], [70, 2000, 3]], ids=["whole", "split"])
+def test_attend_scales_at_the_ends_of_fp32(lens, softmax_scale):
+    # the scale of a block of zeros, and one whose product with softmax_scale is
+    # past fp32; all keys are zeros, so every weight is the same
+    p = Attend(lens, 1, 4, 128, 2, False, seed=30)
+    p.k[:] = 0
+    p.ks[:] = 2.0 ** -126 if softmax_scale < 1 else 2.0 ** 120
+    p.scale = np.float32(softmax_scale)
+    desc = p.desc
+    p.desc = lambda: B.make_gqa_desc(len(lens), 4, 1, 128, p.table.shape[1], p.k.shape[0], softmax_scale=softmax_scale)
+    assert bytes(desc())[:32] == bytes(p.desc())[:32]
+    check(p)
+
+
 def test_attend_nan_codes_stay_with_the_rows_that_see_them():
     # the last chunk token's V holds a NaN: earlier rows of the chunk are whole
     p = Attend([200, 64, 130], 1, 4, 128, 4, False, seed=11)

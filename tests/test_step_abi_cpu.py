@@ -80,6 +80,7 @@ def test_gqa_append_arguments():
     for name in ("slots", "ks", "vs"):
         assert append(desc(), **{name: FAKE + 2}) == MISALIGNED, name
     assert append(desc(), ts=100) == MISALIGNED and append(desc(), hs=4) == MISALIGNED
+    assert append(desc(), n=(1 << 24) + 1) == UNSUPPORTED   # 2 KV heads
     assert append(desc(), n=0, k=None, v=None, slots=None, kp=None, vp=None, ks=None, vs=None) == B.SPLASH_OK
 
 
@@ -116,7 +117,7 @@ def test_rope_arguments():
     assert rope(views=0) == BAD and rope(views=3) == BAD and rope(n=-1) == BAD and rope(heads=-1) == BAD
     assert rope(axes=0) == BAD and rope(axes=5) == BAD and rope(scale=float("nan")) == BAD
     assert rope(rot=63) == UNSUPPORTED and rope(rot=0) == UNSUPPORTED and rope(rot=258) == UNSUPPORTED
-    assert rope(heads=65537) == UNSUPPORTED and rope(n=(1 << 30) + 1) == UNSUPPORTED
+    assert rope(heads=65537) == UNSUPPORTED and rope(n=(1 << 25) + 1) == UNSUPPORTED
     assert rope(freq=[1.0] * 31 + [float("inf")]) == BAD
     assert rope(axis=[0] * 31 + [1]) == BAD and rope(axes=2, axis=[0] * 31 + [2]) == BAD
     assert rope(x=None) == BAD and rope(y=None) == BAD and rope(pos=None) == BAD
