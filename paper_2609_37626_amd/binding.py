@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -128,7 +129,7 @@ _SIGNATURES = {
     "splash_device_workers": (_I32, []),
     "splash_step_tables": (ctypes.c_int, [_VP, _VP, _I32, _I32, _VP, _I32, _VP, _VP, _VP, _I32, _I32, _I32, _VP, _VP, _VP,
                                           _VP, _VP]),
-    "splash_rope": (ctypes.c_int, [ctypes.POINTER(RopeView), _I32, _VP, _I64, _I32, ctypes.POINTER(RopeDesc), _VP]),
+    "splash_rope": (ctypes.c_int, [_VP, _I32, _VP, _I64, _I32, ctypes.POINTER(RopeDesc), _VP]),
     "splash_gqa_append": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _I32, _VP, _VP, _VP, _VP, _PG, _VP]),
     "splash_gqa_workspace_size": (_SZ, [_PG, _I32]),
     "splash_gqa_attend": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _VP, _VP, _PG, _VP, _SZ, _VP]),
@@ -360,14 +361,17 @@ def _refuse(message: str):
     raise SplashError(SPLASH_ERR_INVALID_ARGUMENT, message)
 
 
-_I32T = _F32T = _BF16T = None  # torch's types, and the call that names the device (set by _types)
-_device = None
+_I32T = _F32T = _BF16T = None  # torch's types, and the calls that name the device and its current stream (set by _types)
+_device = _raw_stream = None
+_CODES = {}  # code_type: the types of its pages
 
 
 def _types():
-    global _I32T, _F32T, _BF16T, _device
+    global _I32T, _F32T, _BF16T, _device, _raw_stream
     import torch
     _I32T, _F32T, _BF16T, _device = torch.int32, torch.float32, torch.bfloat16, torch._C._cuda_getDevice
+    _CODES.update({GQA_E4M3: (torch.uint8, torch.float8_e4m3fn), GQA_INT8: (torch.int8,)})
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: _current_stream())
 
 
 def _refuse_tensors(dev: int, **tensors):
@@ -392,7 +396,7 @@ def _refuse_tensors(dev: int, **tensors):
 def _on_device(dev: int, fn, args, stream) -> None:
     """fn(*args, stream handle) with `dev` current."""
     if _device() == dev:
-        status = fn(*args, _stream(stream))
+        status = fn(*args, _raw_stream(dev) if stream is None else _stream(stream))
     else:
         import torch
         with torch.cuda.device(dev):
@@ -480,18 +484,19 @@ def splash_step_tables(seq_lens, q_chunk: int, free_pages, taken_in, taken_out, 
         new_indptr.data_ptr(), slots.data_ptr(), positions.data_ptr(), requests.data_ptr()), stream)
 
 
-def _rope_view(view: RopeView, x, y, tokens: int, rot_dim: int, dev: int) -> None:
+# Two splash_rope_view (a ctypes array takes 1 us longer to fill).
+_pack_views = struct.Struct("@PPqqqqi4xPPqqqqi4x").pack
+_NO_VIEW = (0,) * 7
+
+
+def _rope_view(x, y, tokens: int, rot_dim: int, dev: int) -> tuple:
     shape = x.shape
     xs, ys = x.stride(), y.stride()
     if not (x.dtype is _BF16T and y.dtype is _BF16T and x.get_device() == dev == y.get_device() and len(shape) == 3
             and shape == y.shape and shape[0] == tokens and shape[2] == rot_dim and xs[2] == 1 == ys[2]):
         _refuse(f"x and out must be bf16 [{tokens}, heads, {rot_dim}] on the positions' device, the last dimension dense "
                 f"(got {x.dtype}, {y.dtype}, {tuple(shape)}, {tuple(y.shape)}, strides {xs}, {ys})")
-    view.x = x.data_ptr()
-    view.y = y.data_ptr()
-    view.num_heads = shape[1]
-    view.x_token_stride, view.x_head_stride, _ = xs
-    view.y_token_stride, view.y_head_stride, _ = ys
+    return x.data_ptr(), y.data_ptr(), xs[0], xs[1], ys[0], ys[1], shape[1]
 
 
 def splash_rope(x, positions, rope: RopeDesc, out=None, x2=None, out2=None, stream=None) -> None:
@@ -503,31 +508,26 @@ def splash_rope(x, positions, rope: RopeDesc, out=None, x2=None, out2=None, stre
     axes, n = (1, shape[0]) if len(shape) == 1 else shape if len(shape) == 2 else (0, 0)
     if axes != rope.num_axes or positions.dtype is not _I32T or (n > 1 and strides[-1] != 1) or dev < 0:
         _refuse(f"positions must be int32 [{rope.num_axes}, tokens] on the GPU, dense along the tokens")
-    views = (RopeView * 2)()
     rot = rope.rot_dim
-    _rope_view(views[0], x, x if out is None else out, n, rot, dev)
-    if x2 is not None:
-        _rope_view(views[1], x2, x2 if out2 is None else out2, n, rot, dev)
+    views = _pack_views(*_rope_view(x, x if out is None else out, n, rot, dev),
+                        *(_NO_VIEW if x2 is None else _rope_view(x2, x2 if out2 is None else out2, n, rot, dev)))
     _on_device(dev, lib().splash_rope, (views, 1 if x2 is None else 2, positions.data_ptr(), strides[0] if axes > 1 else n,
                                         n, rope), stream)
 
 
 def _gqa_cache_ok(desc: GqaDesc, dev: int, k_pages, v_pages, k_scales, v_scales) -> bool:
     scales, code = (desc.num_pages, desc.num_kv_heads), k_pages.dtype
-    pool = scales + (64, desc.head_dim)
+    pool = (*scales, 64, desc.head_dim)
     return (k_pages.shape == pool and v_pages.shape == pool and k_scales.shape == scales and v_scales.shape == scales
-            and code is v_pages.dtype and code in _code_types(desc) and k_scales.dtype is _F32T and v_scales.dtype is _F32T
+            and code is v_pages.dtype and code in _CODES.get(desc.code_type, ()) and k_scales.dtype is _F32T and v_scales.dtype is _F32T
             and k_pages.is_contiguous() and v_pages.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()
             and 0 <= dev == k_pages.get_device() == v_pages.get_device() == k_scales.get_device() == v_scales.get_device())
 
 
-def _code_types(desc: GqaDesc):
-    import torch
-    return (torch.uint8, torch.float8_e4m3fn) if desc.code_type == GQA_E4M3 else (torch.int8,)
-
-
 def _refuse_gqa(desc: GqaDesc, dev: int, k_pages, v_pages, k_scales, v_scales, **tensors):
-    scales, codes = (desc.num_pages, desc.num_kv_heads), _code_types(desc)
+    scales, codes = (desc.num_pages, desc.num_kv_heads), _CODES.get(desc.code_type, ())
+    if not codes:
+        _refuse(f"unknown code_type {desc.code_type}")
     pool = scales + (64, desc.head_dim)
     _refuse_tensors(dev, k_pages=(k_pages, codes, pool), v_pages=(v_pages, codes, pool),
                     k_scales=(k_scales, (_F32T,), scales), v_scales=(v_scales, (_F32T,), scales), **tensors)
