@@ -3,13 +3,14 @@
 //
 // A tile is one request, one KV head and 16 to 128 of its query rows (q_chunk
 // rows times the heads that share the KV head): every K and V byte is read once
-// for all of them.  The tiles' pages, one tile after the other with
+// for all of them (by two groups of waves where the rows take two).  A step is
+// the pages that a group's waves take side by side, one each: four, or two for
+// the larger row counts.  The tiles' steps, one tile after the other with
 // kGqaTileCost places in front of each for its fixed work, form one line, which is
 // cut into equal spans, one for each workgroup: long and short histories load
 // the chip alike without a plan, and only the tiles that a cut goes through
 // leave partial results, at most two a workgroup, which a second kernel joins.
-// A workgroup's four waves take the pages of a span's tile in turn, one a step,
-// and join their results through LDS.  Nothing else goes through LDS: each
+// The waves' results of a piece are joined through LDS.  Nothing else goes through LDS: each
 // operand is loaded from the cache in the layout that its MFMA reads, because
 // the contraction's order is free as long as both operands agree on it.
 //   QK  S^T[key, row] = K Q^T, v_mfma_f32_16x16x32_bf16.  Lane (g, c), g =
@@ -47,10 +48,12 @@ constexpr float kMoveAt = 8.f;        // the reference moves once a score passes
 constexpr float kNegInf = -__builtin_inff();
 
 // Places of a tile in the line: kGqaTileCost for its fixed work (two to three
-// steps' time: first loads, queries, the join; a ragged batch of 64 took 104 us
-// with 2, 90 with 4, 74 with 6, 68 with 8, 65 with 12, where 256 short ones lost
-// 1%), then its pages.  A span is at least kLeastSpan places long.
-constexpr int kLeastSpan = 6;
+// steps' time: first loads, queries, the join; a ragged batch of 64 takes 61 us
+// with 2 or 3 and 62.5 with 4, 256 short histories 234.5 with 2, 236 with 3 and
+// 238 with 4; with no such places the ragged batch took half as long again), then
+// its steps (cut between any two pages the ragged batch took 63).  A span is at
+// least kLeastSpan places long.
+constexpr int kLeastSpan = 3;
 
 // ---- codes to MFMA operands (exact) --------------------------------------
 
@@ -157,11 +160,13 @@ struct Shape {
   static constexpr int kKDw = D / 16;         // dwords of a lane's share of a K row (D/4 bytes)
   static constexpr int kVDw = D / 64;         // dwords of a lane's share of a V row (D/16 bytes)
   static constexpr int kDims = D / 16;        // dims of a lane's share, = MFMA row groups of O^T
-  // Workgroups on a CU: two with 256 registers a wave, or one with 512. Two where
-  // the kernel fits 256 without going to memory for them (64 dims with 64 rows:
-  // 52 us against 65 for 64 histories of 2,048 to 8,192), one for the larger (128
-  // dims with 32 rows, which does not: 62 us against 68 for a ragged batch).
-  static constexpr int kPerCu = D * MT <= 128 || D == 64 ? 2 : 1;
+  // Workgroups on a CU: two with 256 registers a wave, or one with 512. Two for 64
+  // dims, whose waves have too few bytes on the way alone (64 rows and 64
+  // histories of 2,048 to 8,192: 52 us against 63; 32 rows 33 against 40), one for
+  // the larger, which has half the spans to begin and join (128 dims with 16 rows
+  // and 256 histories of 1,024 to 4,096: 226 us against 234; with 32 rows, which
+  // two do not hold in registers, a ragged batch 59 against 71).
+  static constexpr int kPerCu = D == 64 ? 2 : 1;
   // the waves' results are joined kPass dims of each share at a time
   static constexpr int kJoinBytes = kPerCu == 2 ? 65536 : 131072;
   static constexpr int kPass = (kWaves * kWaveRows * D * 4 <= kJoinBytes) ? kDims : kJoinBytes / (kWaves * kWaveRows * 64);
@@ -193,6 +198,8 @@ __device__ __forceinline__ int history(const GqaAttendLaunch& a, int b) {
   return seq < 0 ? 0 : (seq > most ? most : seq);
 }
 __device__ __forceinline__ int pages_of(int seq) { return (seq + kPage - 1) / kPage; }
+template <int LANES>
+__device__ __forceinline__ int places_of(int seq) { return kGqaTileCost + (pages_of(seq) + LANES - 1) / LANES; }
 
 // A workgroup's share of one tile: pages [p0, p1) of request b's KV head hk for
 // the query rows from row0 on.  slot: -1 for a whole tile, else the partial
@@ -209,13 +216,14 @@ struct Walk {
 // The workgroup's span of the line: every thread sums a few requests' places, a
 // scan over the workgroup gives the line's length and with it the spans, and
 // the thread whose requests hold the span's start finds the request.
+template <int LANES>
 __device__ __forceinline__ Walk find_span(const GqaAttendLaunch& a, int tiles, int* lds) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int per = (a.B + 64 * kWaves - 1) / (64 * kWaves);
   int mine = 0;
   for (int k = 0; k < per; ++k) {
     const int b = t * per + k;
-    if (b < a.B) mine += tiles * (pages_of(history(a, b)) + kGqaTileCost);
+    if (b < a.B) mine += tiles * places_of<LANES>(history(a, b));
   }
   int upto = mine;
 #pragma unroll
@@ -235,7 +243,7 @@ __device__ __forceinline__ Walk find_span(const GqaAttendLaunch& a, int tiles, i
   if (lo < hi && lo >= upto - mine && lo < upto) {
     int start = upto - mine;
     for (int b = t * per;; ++b) {
-      const int next = start + tiles * (pages_of(history(a, b)) + kGqaTileCost);
+      const int next = start + tiles * places_of<LANES>(history(a, b));
       if (lo < next) {
         lds[kWaves] = b;
         lds[kWaves + 1] = start;
@@ -253,14 +261,15 @@ __device__ __forceinline__ Walk find_span(const GqaAttendLaunch& a, int tiles, i
           {-1, 0, 0, 0}};
 }
 
+template <int LANES>
 __device__ __forceinline__ bool next_piece(const GqaAttendLaunch& a, int row_blocks, int rows_per_tile, Walk& w, Piece* out) {
   const int tiles = a.Hk * row_blocks;
   while (w.at < w.hi) {
-    const int seq = history(a, w.b), pages = pages_of(seq), cost = pages + kGqaTileCost;
+    const int seq = history(a, w.b), pages = pages_of(seq), cost = places_of<LANES>(seq);
     const int tile = __builtin_amdgcn_readfirstlane((w.at - w.b_start) / cost), start = w.b_start + tile * cost;
     const int hk = __builtin_amdgcn_readfirstlane(tile / row_blocks), rb = tile - hk * row_blocks;
     const bool begins = w.at == start;
-    int p0 = max(w.at - start - kGqaTileCost, 0), p1 = max(min(w.hi - start - kGqaTileCost, pages), 0);
+    int p0 = max(w.at - start - kGqaTileCost, 0) * LANES, p1 = max(min((w.hi - start - kGqaTileCost) * LANES, pages), 0);
     if (a.whole_tiles) {
       p0 = begins ? 0 : pages;
       p1 = pages;
@@ -274,7 +283,7 @@ __device__ __forceinline__ bool next_piece(const GqaAttendLaunch& a, int row_blo
     // (a tile without a page belongs to the span of its first place)
     if (p0 < p1 || (pages == 0 && begins)) {
       if (p0 == 0 && p1 < pages)
-        w.joined = {piece.b, hk, rb, (start + kGqaTileCost + pages - 1) / w.chunk - (int)blockIdx.x + 1};
+        w.joined = {piece.b, hk, rb, (start + cost - 1) / w.chunk - (int)blockIdx.x + 1};
       *out = piece;
       return true;
     }
@@ -381,9 +390,9 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
   const int wave_row = wave / S::kLanes * S::kWaveRows;  // first row in the tile
   const int rows = a.q_chunk * a.group, Hq = a.Hk * a.group;
   const int row_blocks = (rows + S::kRows - 1) / S::kRows;
-  Walk walk = find_span(a, a.Hk * row_blocks, lds_span);
+  Walk walk = find_span<S::kLanes>(a, a.Hk * row_blocks, lds_span);
   Piece t, next_t;
-  bool more = next_piece(a, row_blocks, S::kRows, walk, &t);
+  bool more = next_piece<S::kLanes>(a, row_blocks, S::kRows, walk, &t);
   if (!more) {
     if (threadIdx.x == 0) a.joined[blockIdx.x] = walk.joined;
     return;
@@ -436,7 +445,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
   load_q(t);
   load_k(block);
   while (true) {
-    more = next_piece(a, row_blocks, S::kRows, walk, &next_t);
+    more = next_piece<S::kLanes>(a, row_blocks, S::kRows, walk, &next_t);
     if (!more) next_t = t;
     const int pages = t.p0 + turn < t.p1 ? (t.p1 - t.p0 - turn + S::kLanes - 1) / S::kLanes : 0;  // of this wave
     if (pages == 1) next = entry(next_t, 0);
@@ -689,7 +698,7 @@ hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
   const int64_t row_blocks = ((int64_t)a.q_chunk * a.group + S::kRows - 1) / S::kRows;
   a.workers = a.workers * S::kPerCu < kGqaMaxWorkers ? a.workers * S::kPerCu : kGqaMaxWorkers;
   // no more workgroups than the longest histories would fill
-  const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * (a.bt_stride + kGqaTileCost) + kLeastSpan - 1) / kLeastSpan;
+  const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * ((a.bt_stride + S::kLanes - 1) / S::kLanes + kGqaTileCost) + kLeastSpan - 1) / kLeastSpan;
   if (a.workers > most) a.workers = (int32_t)most;
   // Few short tiles are not cut: each goes to the span that it begins in, and
   // there is nothing to join (8 tiles of 2 to 8 pages: one launch of 8 us instead

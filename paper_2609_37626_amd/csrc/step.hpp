@@ -79,7 +79,7 @@ struct GqaAttendLaunch {
 };
 
 constexpr int32_t kGqaMaxWorkers = 512;
-constexpr int32_t kGqaTileCost = 8;  // a tile's fixed work, in pages
+constexpr int32_t kGqaTileCost = 2;  // a tile's fixed work, in steps of its waves
 
 // Query rows of a tile, for `rows` of them per KV head: the fewest that hold
 // them, at most 128 (64 at 256 dims, whose accumulators take twice the registers).
