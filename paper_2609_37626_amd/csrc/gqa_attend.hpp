@@ -10,9 +10,9 @@
 // cut into equal spans, one for each workgroup: long and short histories load
 // the chip alike without a plan, and only the tiles that a cut goes through
 // leave partial results, at most two a workgroup, which a second kernel joins.
-// The waves' results of a piece are joined through LDS.  Nothing else goes through LDS: each
-// operand is loaded from the cache in the layout that its MFMA reads, because
-// the contraction's order is free as long as both operands agree on it.
+// The waves' results of a piece are joined through LDS; nothing else goes through
+// it: each operand is loaded from the cache in the layout that its MFMA reads,
+// because the contraction's order is free as long as both operands agree on it.
 //   QK  S^T[key, row] = K Q^T, v_mfma_f32_16x16x32_bf16.  Lane (g, c), g =
 //       lane / 16, c = lane % 16, holds dims [64 i + 16 g, + 16) of key c for
 //       every i, so that the four lanes of a key read whole 64-byte pieces; Q is
@@ -24,7 +24,7 @@
 // The weights 2^(z - m + 6) are taken against a reference m that moves only
 // when a row's maximum passes it by 2^8, so a weight stays below 2^14 and no
 // exchange between lanes is needed on the other steps; 2^6 keeps the small ones
-// off fp16's subnormals.  P is rounded to fp16 (2^-12 relative) for PV.  A
+// off fp16's subnormals.  P is rounded to fp16 (2^-11 relative) for PV.  A
 // block's V scale multiplies its product in fp32, never the weights.
 //
 // Bound: HBM.  A page costs 128 D bytes against 4 D x 64 x 16 MT flops.
@@ -124,9 +124,10 @@ struct Dwords {
 };
 // `at` is uniform and `lane` the lane's own offset, so that the address takes one register.
 // Non-temporal where 16 lanes read whole 128-byte lines (V up to 128 dims),
-// each once: four histories of 65,536 to 131,072 tokens 125 -> 114 us. Not for
-// the 16-byte pieces, whose lines a later load or another wave reads again: with
-// both non-temporal 242 us instead of 233 for 256 histories of 1,024 to 4,096.
+// each once: 256 histories of 1,024 to 4,096 tokens 248 -> 226 us, four of 65,536
+// to 131,072 124 -> 112. Not for the 16-byte pieces, whose lines a later load or
+// another wave reads again: with both non-temporal 233 us for the 256 (109 for the
+// four), and 93 instead of 83 for 64 rows of 256 dims.
 // Pieces of 16 bytes lie `step` bytes apart.
 template <int N>
 __device__ __forceinline__ Dwords<N> load_dwords(const uint8_t* at, uint32_t lane, int step = 16) {
@@ -701,7 +702,7 @@ hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
   const int64_t most = ((int64_t)a.B * a.Hk * row_blocks * ((a.bt_stride + S::kLanes - 1) / S::kLanes + kGqaTileCost) + kLeastSpan - 1) / kLeastSpan;
   if (a.workers > most) a.workers = (int32_t)most;
   // Few short tiles are not cut: each goes to the span that it begins in, and
-  // there is nothing to join (8 tiles of 2 to 8 pages: one launch of 8 us instead
+  // there is nothing to join (8 tiles of 2 to 8 pages: one launch of 7 us instead
   // of 7 and 4). At 16 pages a wave has four.
   a.whole_tiles = a.bt_stride <= 16 && (int64_t)a.B * a.Hk * row_blocks <= a.workers;
   hipLaunchKernelGGL((gqa_attend_kernel<D, MT, RG, CODE>), dim3(a.workers), dim3(64 * kWaves), 0, s, a);
