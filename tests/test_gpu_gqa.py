@@ -54,6 +54,17 @@ def test_attend_long_chunks(dim, q_chunk, lens):
     check(Attend(lens, 1, 2, dim, q_chunk, False, seed=29).poison(), f"d{dim} q{q_chunk}")
 
 
+@pytest.mark.parametrize("dim,kv_heads,group", [(64, 1, 4), (256, 1, 2)])
+def test_attend_one_history_over_the_whole_chip(dim, kv_heads, group):
+    # (more parts of a tile than a wave of the join has lanes)
+    check(Attend([120000], kv_heads, group, dim, 1, False, seed=31).poison())
+
+
+@pytest.mark.parametrize("kv_heads,group,dim,q_chunk", [(1, 1024, 128, 1), (128, 8, 64, 1), (128, 1, 256, 2), (2, 300, 64, 2)])
+def test_attend_most_heads(kv_heads, group, dim, q_chunk):
+    check(Attend([130, 0, 1300], kv_heads, group, dim, q_chunk, False, seed=32).poison())
+
+
 def test_attend_many_requests():
     rng = np.random.Generator(np.random.PCG64(5))
     check(Attend(rng.integers(0, 200, 700), 2, 4, 64, 1, False, seed=8).poison())
