@@ -629,15 +629,18 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
   if (threadIdx.x == 0) a.joined[blockIdx.x] = walk.joined;
 }
 
-// Joins the parts of the tile whose first part workgroup blockIdx.x of the
+// Joins the parts of the tile whose first part workgroup blockIdx.y of the
 // attend kernel has, if any: one wave per row.  The parts lie in slots 2w + 1,
 // 2(w + 1), 2(w + 2), ...; lanes take 4 dims each, 64 / (D / 4) parts at a time.
+// (Rows along x: equal histories begin in every n-th workgroup, and along x those
+// would all run on one XCD where n is a multiple of 8; 32 tiles of 64 rows by 256
+// dims in eight parts 8.5 -> 7.0 us.)
 template <int D, int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void gqa_join_kernel(GqaAttendLaunch a) {
-  const int w = blockIdx.x, lane = threadIdx.x & 63;
+  const int w = blockIdx.y, lane = threadIdx.x & 63;
   const int4 tile = a.joined[w];
   if (tile.x < 0) return;
-  const int rr = blockIdx.y * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rr = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = tile.z * ROWS + rr;
   if (r >= a.q_chunk * a.group) return;
   const int parts = tile.w;
@@ -708,7 +711,7 @@ hipError_t launch_shape(GqaAttendLaunch a, hipStream_t s) {
   hipLaunchKernelGGL((gqa_attend_kernel<D, MT, RG, CODE>), dim3(a.workers), dim3(64 * kWaves), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.whole_tiles) return e;
-  hipLaunchKernelGGL((gqa_join_kernel<D, S::kRows>), dim3(a.workers, S::kRows / kWaves), dim3(64 * kWaves), 0, s, a);
+  hipLaunchKernelGGL((gqa_join_kernel<D, S::kRows>), dim3(S::kRows / kWaves, a.workers), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
 
