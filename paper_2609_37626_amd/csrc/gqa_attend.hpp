@@ -357,7 +357,10 @@ __device__ __forceinline__ void join_waves(const GqaAttendLaunch& a, const Piece
         }
     __syncthreads();
     constexpr int kQuads = 4 * S::kPass;  // 4-float pieces of a row in this pass
-    for (int e = threadIdx.x; e < S::kRows * kQuads; e += 64 * kWaves) {
+    static_assert(S::kRows * kQuads % (64 * kWaves) == 0, "whole turns");
+#pragma unroll 8
+    for (int turn = 0; turn < S::kRows * kQuads / (64 * kWaves); ++turn) {
+      const int e = turn * 64 * kWaves + threadIdx.x;
       const int rr = e / kQuads, k4 = e - rr * kQuads;
       f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
