@@ -160,9 +160,9 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
   if (st != SPLASH_OK) return st;
   if (num_tokens < 0 || token_stride < 0 || head_stride < 0)
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_tokens and strides must be >= 0");
+  if (num_tokens == 0 || desc->batch == 0) return SPLASH_OK;
   if ((int64_t)num_tokens * desc->num_kv_heads > kMaxAppendRows)
     return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens * num_kv_heads passes 2^25");
-  if (num_tokens == 0 || desc->batch == 0) return SPLASH_OK;
   if (!k_new || !v_new || !slots) return fail(SPLASH_ERR_INVALID_ARGUMENT, "k_new, v_new and slots must be non-NULL");
   if ((st = check_gqa_cache(k_pages, v_pages, k_scales, v_scales)) != SPLASH_OK) return st;
   if (!aligned(k_new, 16) || !aligned(v_new, 16) || token_stride % 8 || head_stride % 8)

@@ -81,6 +81,7 @@ def test_gqa_append_arguments():
         assert append(desc(), **{name: FAKE + 2}) == MISALIGNED, name
     assert append(desc(), ts=100) == MISALIGNED and append(desc(), hs=4) == MISALIGNED
     assert append(desc(), n=(1 << 24) + 1) == UNSUPPORTED   # 2 KV heads
+    assert append(desc(batch=0), n=(1 << 24) + 1) == B.SPLASH_OK
     assert append(desc(), n=0, k=None, v=None, slots=None, kp=None, vp=None, ks=None, vs=None) == B.SPLASH_OK
 
 
