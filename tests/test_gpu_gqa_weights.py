@@ -1,0 +1,77 @@
+"""splash_gqa_attend where softmax weights and V block scales lie far apart and decide the result together."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from paper_2609_37626_amd import binding as B
+from paper_2609_37626_amd.workloads import f32_to_bf16_bits
+from tests.step_inputs import PAGE, Attend, assert_close
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+def levelled(lens, kv_heads, group, dim, q_chunk, int8, seed, levels):
+    """Page p of a history holds scores of about levels(p) powers of two, and its V block a scale of 2^-levels(p), so
+    that every page has a like part in the output.  Dim 0 carries the level: queries 32 there, codes level by level."""
+    rng = np.random.Generator(np.random.PCG64(seed))
+    p = Attend(lens, kv_heads, group, dim, q_chunk, int8, seed)
+    n, hq, d = len(lens) * q_chunk, kv_heads * group, dim
+    q = rng.standard_normal((n, hq, d)).astype(np.float32)
+    q[..., 0] = 32.0
+    p.q = f32_to_bf16_bits(q)
+    per_code = 32.0 * 2.0 ** -3 * float(p.scale) * np.log2(np.e)  # powers of two of one unit of the code in dim 0
+    top = 120 if int8 else 448
+    p.ks[:] = 2.0 ** -3
+    for x, lo, hi in ((p.k, -2, 2), (p.v, 32, 120)):   # (V: no code is small beside its block's largest)
+        vals = rng.integers(lo, hi, x.shape, endpoint=True) * rng.choice([-1.0, 1.0], x.shape)
+        x[:] = oracle.step.encode(vals, int8)
+    for row, s in zip(p.table, lens):
+        for at in range(-(-s // PAGE)):
+            code = np.clip(np.round(levels(at) / per_code), -top, top)
+            p.k[row[at], :, :, 0] = oracle.step.encode(np.full((kv_heads, PAGE), code), int8)
+            held = oracle.step.decode(p.k[row[at], :1, :1, 0], int8)[0, 0] * per_code
+            p.vs[row[at]] = 2.0 ** -round(held)
+    return p
+
+
+def check(p, label):
+    out, lse = p.attend()
+    ref = p.oracle()
+    # The bound of a plain problem holds: with no V code small beside its block's
+    # largest, what a block's weights lose below 2^-40 of its largest weight is
+    # far under the 2^-11 of the weighted |V| that it counts.
+    assert_close(out, lse, ref, int(max(p.lens)), p.dim, label)
+    assert np.abs(ref[0]).max() > 0
+
+
+@pytest.mark.parametrize("int8", [False, True], ids=["e4m3", "int8"])
+@pytest.mark.parametrize("order", ["falling", "rising", "mixed"])
+@pytest.mark.parametrize("dim,group,q_chunk", [(64, 4, 1), (64, 9, 8), (128, 8, 1), (128, 8, 4), (128, 16, 8), (256, 2, 1), (256, 8, 8)])
+def test_attend_low_scores_under_large_v_scales(int8, order, dim, group, q_chunk):
+    # a page of one wave every fourth (or second): levels 33 powers apart from one to its next
+    levels = {"falling": lambda at: 33 - 66 * (at // 4 % 2), "rising": lambda at: 66 * (at // 4 % 2) - 33,
+              "mixed": lambda at: (at * 37) % 64 - 32}[order]
+    check(levelled([300, 700, 64, 5], 2, group, dim, q_chunk, int8, seed=dim + group, levels=levels), f"d{dim} g{group} q{q_chunk} {order}")
+
+
+@pytest.mark.parametrize("int8", [False, True], ids=["e4m3", "int8"])
+def test_attend_low_scores_under_large_v_scales_over_many_workgroups(int8):
+    # (tiles cut between workgroups, and parts of them joined)
+    check(levelled([9000, 3000, 130], 1, 8, 128, 2, int8, seed=3, levels=lambda at: (at * 29) % 44 - 22), "split")
+
+
+@pytest.mark.parametrize("int8", [False, True], ids=["e4m3", "int8"])
+def test_attend_two_pages_of_one_wave(int8):
+    # page 4 after page 0 in one wave: scores 32 powers of two down, V's scale 2^31 up: a third of the output
+    p = levelled([5 * PAGE], 1, 1, 64, 1, int8, seed=4, levels=lambda at: 16 if at == 0 else -16 if at == 4 else -80)
+    p.vs[:] = 2.0 ** -31
+    p.vs[p.table[0, 4]] = 1.0
+    check(p, "two pages")
