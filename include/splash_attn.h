@@ -456,15 +456,17 @@ int splash_step_tables(const int32_t* seq_lens, const int32_t* new_lens, int32_t
  *   view   x, y: bf16, element d of head h of token n at
  *          n * token_stride + h * head_stride + d (strides in elements, of x
  *          and y each); y == x with the same strides rotates in place, else
- *          the two must not overlap, and no y another view.  Only rot_dim elements of a head are read
- *          and written.
+ *          the two must not overlap, and no y another view.  Rows of one y that
+ *          overlap are refused (of one x they may, where y is elsewhere), and so
+ *          is a y that begins where the other view's x or y does.  Only rot_dim
+ *          elements of a head are read and written.
  *   positions  int32, axis a's position of token n at [a * position_stride + n];
  *          where num_axes > 1, position_stride >= num_tokens, or 0 (text: every
  *          axis has the same positions)
  * inv_freq and pair_axis are HOST arrays of rot_dim / 2, read during the call.
  * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, num_axes outside
  * 1 .. 4, an axis outside [0, num_axes), an inv_freq or scale that is not
- * finite), UNSUPPORTED (rot_dim odd or outside 2 .. 256, more than 65536
+ * finite, overlapping rows or views as above), UNSUPPORTED (rot_dim odd or outside 2 .. 256, more than 65536
  * heads or 2^25 tokens), MISALIGNED (x or y not 2-byte, positions not 4-byte aligned).
  */
 typedef struct splash_rope_view {

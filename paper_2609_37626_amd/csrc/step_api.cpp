@@ -56,6 +56,22 @@ int check_gqa_cache(const void* k_pages, const void* v_pages, const float* k_sca
   return SPLASH_OK;
 }
 
+// Whether two of a view's rows, `width` elements at n * token + h * head, share
+// an element.  Rows n tokens apart in one direction and h heads in the other lie
+// |h * head - n * token| apart; of each h the two nearest n decide.
+bool rows_overlap(int64_t tokens, int64_t token, int64_t heads, int64_t head, int64_t width) {
+  if ((tokens > 1 && token < width) || (heads > 1 && head < width)) return true;
+  if (tokens < 2 || heads < 2) return false;
+  typedef __int128 Wide;
+  if ((Wide)token >= (Wide)(heads - 1) * head + width || (Wide)head >= (Wide)(tokens - 1) * token + width) return false;
+  for (int64_t h = 1; h < heads; ++h) {
+    const Wide at = (Wide)h * head, n = at / token, past = at - n * token;
+    if (n >= tokens) return false;
+    if (past < width || (n + 1 < tokens && token - past < width)) return true;
+  }
+  return false;
+}
+
 struct GqaLayout {
   size_t part_ml, part_out, total;  // the joined tiles' records come first
 };
@@ -136,8 +152,8 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
     if (num_tokens > 0 && w.num_heads > 0) {
       if (!w.x || !w.y) return fail(SPLASH_ERR_INVALID_ARGUMENT, "x and y must be non-NULL");
       if (!aligned(w.x, 2) || !aligned(w.y, 2)) return fail(SPLASH_ERR_MISALIGNED, "x and y must be 2-byte aligned");
-      if ((w.num_heads > 1 && w.y_head_stride < desc->rot_dim) || (num_tokens > 1 && w.y_token_stride < desc->rot_dim))
-        return fail(SPLASH_ERR_INVALID_ARGUMENT, "a stride of y is below rot_dim: its rows overlap");
+      if (rows_overlap(num_tokens, w.y_token_stride, w.num_heads, w.y_head_stride, desc->rot_dim))
+        return fail(SPLASH_ERR_INVALID_ARGUMENT, "rows of y overlap");
       if (w.x == w.y && (w.x_token_stride != w.y_token_stride || w.x_head_stride != w.y_head_stride))
         return fail(SPLASH_ERR_INVALID_ARGUMENT, "rotating in place needs equal strides");
     }
@@ -145,6 +161,9 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
                  w.y_token_stride, w.y_head_stride, w.num_heads};
   }
   if (num_tokens == 0) return SPLASH_OK;
+  if (num_views == 2 && views[0].num_heads > 0 && views[1].num_heads > 0 &&
+      (views[0].y == views[1].y || views[0].y == views[1].x || views[1].y == views[0].x))
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "a view's y is the other view's x or y");
   if (!positions) return fail(SPLASH_ERR_INVALID_ARGUMENT, "positions is NULL");
   if (!aligned(positions, 4)) return fail(SPLASH_ERR_MISALIGNED, "positions not 4-byte aligned");
   if (desc->num_axes > 1 && position_stride < num_tokens && position_stride != 0)
