@@ -369,9 +369,10 @@ _CODES = {}  # code_type: the types of its pages
 def _types():
     global _I32T, _F32T, _BF16T, _device, _raw_stream
     import torch
-    _I32T, _F32T, _BF16T, _device = torch.int32, torch.float32, torch.bfloat16, torch._C._cuda_getDevice
+    _I32T, _F32T, _BF16T = torch.int32, torch.float32, torch.bfloat16
     _CODES.update({GQA_E4M3: (torch.uint8, torch.float8_e4m3fn), GQA_INT8: (torch.int8,)})
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: _current_stream())
+    _device = torch._C._cuda_getDevice  # (the calls look at this one: last, for their first use from several threads)
 
 
 def _refuse_tensors(dev: int, **tensors):
