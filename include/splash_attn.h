@@ -535,9 +535,9 @@ int splash_gqa_append(const void* k_new, const void* v_new, int64_t token_stride
  *              what it holds is of one call, and calls that may overlap (other
  *              streams, graphs replayed side by side) take one each
  * Codes are converted exactly (K to bf16, V to fp16), products are summed in
- * fp32; a weight is rounded to fp16 before it meets V, and its sum is not.  The
- * rounding is 2^-11 of the weight, or, where it lies 2^-29 and more below the
- * row's largest weight in the same page, 2^-40 of that largest: a page whose
+ * fp32.  A weight meets V in fp16 and its sum does not: to 2^-22 where
+ * q_chunk * num_heads / num_kv_heads is at most 16, else to 2^-11, or 2^-40 of
+ * the row's largest weight in the same page where that is more.  A page whose
  * weights are down to 2^-117 of the row's largest keeps its part in out, however
  * far apart the scales of V lie.
  * Codes of places that no row of the request sees are not used, NaN codes

@@ -22,9 +22,10 @@
 //       those are the keys it contracts; V^T's lane loads dims [c D/16,
 //       (c+1) D/16) of the same keys, and a byte permutation pairs its keys.
 // A page's weights 2^(z - peak + 15) are taken against the row's own largest score
-// in it, `peak`, and rounded to fp16 for PV: 2^-11 relative down to 2^-29 of the
-// largest, 2^-40 of it below (its subnormals), whatever came before and whatever
-// the scales of V are.  The page's products and the sum of its weights meet the
+// in it, `peak`, and go to fp16 for PV, in two terms (2^-22 relative) for tiles of
+// 16 rows and in one (2^-11 relative, down to 2^-29 of the largest) for more; what
+// is below fp16's subnormals, 2^-40 of the largest weight, is lost, whatever came
+// before and whatever the scales of V are.  The page's products and the sum of its weights meet the
 // accumulators in fp32, times 2^(peak - m - 9) and, the products, the block's V
 // scale.  The reference m moves only when a row's score passes it by 2^8, so that
 // the accumulators are seldom multiplied; they stay below 2^14 a key.  (Weights
@@ -173,6 +174,12 @@ struct Shape {
   static constexpr int kKDw = D / 16;         // dwords of a lane's share of a K row (D/4 bytes)
   static constexpr int kVDw = D / 64;         // dwords of a lane's share of a V row (D/16 bytes)
   static constexpr int kDims = D / 16;        // dims of a lane's share, = MFMA row groups of O^T
+  // fp16 terms of a weight.  Two (2^-22) where the second's matrix instructions
+  // hide behind HBM: 16 rows, 237 us with either for 256 histories of 1,024 to
+  // 4,096, 73.3 and 73.5 for 64 of 2,048 to 8,192 at 256 dims; one (2^-11, beside
+  // the output's 2^-8) where they would not: 32 rows of 128 dims 67.5 us with one
+  // and 70 with two, 64 rows of 256 dims 90 and 102, 128 rows of 64 dims 41 and 49.
+  static constexpr int kTerms = MT == 1 ? 2 : 1;
   // Workgroups on a CU: two with 256 registers a wave, or one with 512. Two for 64
   // dims, whose waves have too few bytes on the way alone (64 rows and 64
   // histories of 2,048 to 8,192: 52 us against 63; 32 rows 33 against 40), one for
@@ -524,7 +531,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
       }
 
       // weights (ks brings the products to base-2 scores)
-      uint32_t w[MT][2][4];
+      uint32_t w[MT][S::kTerms][2][4];
       float v_by[MT];  // what brings a row's products to its reference: 2^(peak - m) and V's scale
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
@@ -553,8 +560,17 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
             e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[kt][mt][i], ks, -ref));
             sum += e[i];
           }
-          w[mt][kt >> 1][2 * (kt & 1)] = pack_f16x2(e[0], e[1]);
-          w[mt][kt >> 1][2 * (kt & 1) + 1] = pack_f16x2(e[2], e[3]);
+#pragma unroll
+          for (int term = 0; term < S::kTerms; ++term)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+              const uint32_t pair = pack_f16x2(e[i], e[i + 1]);
+              w[mt][term][kt >> 1][2 * (kt & 1) + i / 2] = pair;
+              if (term + 1 < S::kTerms) {  // what is left of the weights, exactly
+                e[i] -= (float)__builtin_bit_cast(f16x2, pair)[0];
+                e[i + 1] -= (float)__builtin_bit_cast(f16x2, pair)[1];
+              }
+            }
         }
         l[mt] = __builtin_fmaf(sum, by, l[mt]);
         v_by[mt] = vs * by;
@@ -604,11 +620,13 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
             for (int mt = 0; mt < MT; ++mt) {
               f32x4 t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const u32x4 wf = {w[mt][h][0], w[mt][h][1], w[mt][h][2], w[mt][h][3]};
-                t = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, f[dd][h]),
-                                                           __builtin_bit_cast(f16x8, wf), t, 0, 0, 0);
-              }
+              for (int term = 0; term < S::kTerms; ++term)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const uint32_t(&wf)[4] = w[mt][term][h];
+                  t = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, f[dd][h]),
+                                                             __builtin_bit_cast(f16x8, (u32x4){wf[0], wf[1], wf[2], wf[3]}), t, 0, 0, 0);
+                }
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[j][mt][i] = __builtin_fmaf(v_by[mt], t[i], o[j][mt][i]);
             }

@@ -75,3 +75,27 @@ def test_attend_two_pages_of_one_wave(int8):
     p.vs[:] = 2.0 ** -31
     p.vs[p.table[0, 4]] = 1.0
     check(p, "two pages")
+
+
+@pytest.mark.parametrize("int8", [False, True], ids=["e4m3", "int8"])
+@pytest.mark.parametrize("dim,kv_heads,group", [(64, 2, 4), (128, 1, 16), (128, 8, 1), (256, 2, 8)])
+def test_attend_of_few_rows_keeps_weights_past_fp16(int8, dim, kv_heads, group):
+    """Values that nearly cancel: bf16's half step of a small result does not hide what a weight was rounded by.
+
+    Two fp16 terms hold a weight to 2^-22 (2^-11 of what 2^-11 leaves), where tolerances() counts 2^-11; the rest of
+    its bound stands: bf16's half step, the scores' dz and the sums."""
+    rng = np.random.Generator(np.random.PCG64(60 + dim))
+    p = Attend([2] * 96, kv_heads, group, dim, 1, int8, seed=61 + dim, exponents=(-7, -7))
+    first = rng.integers(8, 40, (kv_heads, dim)) * 2 * rng.choice([-1, 1], (kv_heads, dim))
+    for b in range(96):   # the second token's value is -3/2 of the first's
+        for place, x in ((0, first), (1, -first * 3 // 2)):
+            p.v[p.table[b, 0], :, place] = oracle.step.encode(x.astype(np.float64), int8)
+    out, lse = p.attend()
+    ref = p.oracle()
+    exact, mass, spread = ref[0], ref[2], ref[3]
+    dz = (dim + 6) * 2.0 ** -24 * spread + 2.0 ** -21
+    sums = (2 + 64) * 2.0 ** -24
+    tol = 2.0 ** -8 * np.abs(exact) + (2.0 ** -22 + 2 * dz + 2 * sums)[..., None] * mass * 1.01
+    err = np.abs(out.float().cpu().numpy().astype(np.float64) - exact)
+    assert (2.0 ** -8 * np.abs(exact) < 2.0 ** -13 * mass).any()   # results that cancel are there
+    assert np.all(err <= tol), float((err / tol).max())
