@@ -30,8 +30,8 @@
 // scale.  The reference m moves only when a row's score passes it by 2^8, so that
 // the accumulators are seldom multiplied; they stay below 2^14 a key.  (Weights
 // against m itself lose a page whose scores lie 2^-20 and more below it, however
-// large its V scale is.  Against `peak` costs 1% at 128 and 256 dims and 1.5 to 3% at
-// 64: 64 rows of 64 dims INT8 27.4 us against 26.7.)
+// large its V scale is.  Against `peak` costs 1%: 64 rows of 256 dims 90 us, 89
+// against m.)
 //
 // Bound: HBM.  A page costs 128 D bytes against 4 D x 64 x 16 MT flops.
 #pragma once
@@ -180,13 +180,15 @@ struct Shape {
   // the output's 2^-8) where they would not: 32 rows of 128 dims 67.5 us with one
   // and 70 with two, 64 rows of 256 dims 90 and 102, 128 rows of 64 dims 41 and 49.
   static constexpr int kTerms = MT == 1 ? 2 : 1;
-  // Workgroups on a CU: two with 256 registers a wave, or one with 512. Two for 64
-  // dims, whose waves have too few bytes on the way alone (64 rows and 64
-  // histories of 2,048 to 8,192: 52 us against 63; 32 rows 33 against 40), one for
-  // the larger, which has half the spans to begin and join (128 dims with 16 rows
-  // and 256 histories of 1,024 to 4,096: 226 us against 234; with 32 rows, which
-  // two do not hold in registers, a ragged batch 59 against 71).
-  static constexpr int kPerCu = D == 64 ? 2 : 1;
+  // Workgroups on a CU: two with 256 registers a wave, or one with 512.  Two for 64
+  // dims and up to 32 rows, whose waves have few bytes on the way (256 histories
+  // of 1,024 to 4,096, 8 rows INT8: 137 us, with one 139 to 140; 64 of 2,048 to
+  // 8,192: 16 rows 17.6 and 17.2, 32 rows 20.3 either way).  One for the rest,
+  // which two do not hold without scratch or which have half the spans to begin
+  // and join with one: 64 dims E4M3 with 64 rows 27.5 against 31.4 and with 128 rows
+  // 38.5 against 48 (INT8 27.3 either way, 38.7 against 41.6); 128 dims with 16
+  // rows and 256 histories 238 against 248; with 32 rows, a ragged batch, 68 against 92.
+  static constexpr int kPerCu = D == 64 && MT < 4 ? 2 : 1;
   // the waves' results are joined kPass dims of each share at a time
   static constexpr int kJoinBytes = kPerCu == 2 ? 65536 : 131072;
   static constexpr int kPass = (kWaves * kWaveRows * D * 4 <= kJoinBytes) ? kDims : kJoinBytes / (kWaves * kWaveRows * 64);
