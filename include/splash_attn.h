@@ -378,7 +378,9 @@ int splash_mla_plan_host(const int32_t* seq_lens_host, int32_t q_chunk,
  *   splash_gqa_attend    attention of the step's query rows
  * splash_step_tables and splash_rope serve the MLA calls above as well: the
  * block table and slots are the same, and the rotary part of a packed query
- * row or a latent row is a strided view.
+ * row or a latent row is a strided view.  The MLA calls trust the table: after a
+ * step that found no page for a token (taken_out[1] > 0) the requests that went
+ * short are not theirs to attend.
  *
  * These four calls stay inside their buffers whatever the device data holds:
  * lengths are clamped to the block-table row, a block-table entry or slot
@@ -391,7 +393,8 @@ int splash_mla_plan_host(const int32_t* seq_lens_host, int32_t q_chunk,
  *   k_scales, v_scales  fp32 [num_pages, num_kv_heads], finite and > 0:
  *                       value = code * scale of its block
  * A block's scale as splash_gqa_append writes it is a power of two, so that a
- * growing block is brought to a new scale by shifting its codes' exponents.
+ * growing block is brought to a new scale by shifting its codes' exponents (E4M3
+ * codes that reach the subnormals, and INT8 codes, are rounded again).
  */
 #define SPLASH_GQA_E4M3 0   /* codes: OCP E4M3 ("fn") bytes */
 #define SPLASH_GQA_INT8 1   /* codes: signed bytes */
@@ -497,7 +500,8 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
  *   slots         int32 [num_tokens]; row t goes to place slots[t] % 64 of page
  *                 slots[t] / 64; a slot outside [0, 64 * num_pages) is skipped.
  *                 Slots are distinct, and the rows of one page stand next to
- *                 each other in the list (as splash_step_tables writes them).
+ *                 each other in the list, with no skipped slot between them
+ *                 (as splash_step_tables writes them): two runs of one page race.
  * With TOP = 448 (E4M3) or 127 (INT8), for every block that gets rows:
  *   e   = the least e >= -126 with |x| <= TOP * 2^e for every finite new x;
  *         not below the block's own exponent, unless a new row takes place 0,
@@ -507,7 +511,8 @@ int splash_rope(const splash_rope_view* views, int32_t num_views, const int32_t*
  *   new rows: code = x * 2^-e, rounded to nearest even; infinities take the
  *         largest code of their sign; NaN is E4M3's NaN and INT8's 0
  *   scale = 2^e
- * desc->batch, the step's requests, decides only how the work is laid out.
+ * desc->batch, the step's requests, decides only how the work is laid out (8
+ * slots a request and more, skipped ones among them, are taken for prompts).
  * A block that is continued must have a power-of-two scale (as this call
  * writes it; of another, its exponent alone is used).  Rows of a block past its
  * last new place are not written.

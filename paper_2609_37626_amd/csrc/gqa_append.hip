@@ -271,8 +271,9 @@ __global__ __launch_bounds__(kThreads) void gqa_append_rows_kernel(GqaAppendLaun
 
 // The runs that begin among kWindow tokens, for one side: long ones one after
 // the other, short ones one per lane group.  (Four waves a SIMD: with the
-// registers of five it goes to memory for them, 35 us against 25 for 18,093 rows
-// of 8 heads by 128 dims, floor 23.)
+// registers of five it goes to memory for them, 38 us against 28 for 18,093 rows
+// of 8 heads by 128 dims, floor 23.  At 256 dims the rows in registers leave two: as
+// many bytes, 4 heads by 256, take a quarter longer.)
 template <int D, int CODE>
 __global__ __launch_bounds__(kThreads, (D == 256 ? 1 : 4)) void gqa_append_prompts_kernel(GqaAppendLaunch a) {
   constexpr int kPieces = D / 8, kGroups = 64 / kPieces;
@@ -330,7 +331,9 @@ hipError_t launch_code(const GqaAppendLaunch& a, hipStream_t s) {
   constexpr int kGroups = 512 / D;
   // Tokens a request: 2,048 requests with one each take 6.7 us by rows (25 with
   // the wave's lanes on one head), a prompt of 2,000 takes 10 us by windows (22
-  // by rows).
+  // by rows).  The host knows only the list's length, skipped slots among it: 256
+  // one-token requests padded to fewer than 2,048 slots take 4.2 us, to 2,048 and
+  // more 13.7 (22.5 at 256 dims), by windows.
   const bool prompts = a.num_tokens >= 8 * (int64_t)a.batch;
   const int64_t waves = prompts ? ((int64_t)a.num_tokens + kWindow - 1) / kWindow * 2 * a.Hk
                                 : (int64_t)a.num_tokens * ((2 * a.Hk + kGroups - 1) / kGroups);

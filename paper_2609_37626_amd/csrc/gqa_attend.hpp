@@ -33,7 +33,12 @@
 // large its V scale is.  Against `peak` costs 1%: 64 rows of 256 dims 90 us, 89
 // against m.)
 //
-// Bound: HBM.  A page costs 128 D bytes against 4 D x 64 x 16 MT flops.
+// Bound: HBM for 16 and 32 rows (a page costs 128 D bytes against 4 D x 64 flops a
+// row, RG x 16 MT rows a tile); for more the conversions and matrix instructions of
+// one wave a SIMD.  Every block of a request's rows walks its whole history, what a
+// prompt's earlier rows do not see among it: 2,048 rows of a 2,048-token prompt, 64
+// heads over 8 by 128 dims, take 323 us, 213 TFLOP/s of what they see.
+// (Times in this file are of a call's two launches, in a graph.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -55,11 +60,11 @@ constexpr float kMoveAt = 8.f;        // the reference moves once a score passes
 constexpr float kNegInf = -__builtin_inff();
 
 // Places of a tile in the line: kGqaTileCost for its fixed work (two to three
-// steps' time: first loads, queries, the join; a ragged batch of 64 takes 61 us
-// with 2 or 3 and 62.5 with 4, 256 short histories 234.5 with 2, 236 with 3 and
-// 238 with 4; with no such places the ragged batch took half as long again), then
-// its steps (cut between any two pages the ragged batch took 63).  A span is at
-// least kLeastSpan places long.
+// steps' time: first loads, queries, the join; a ragged batch of 64 takes 67.9 us
+// with 2, 68.8 with 3 and 69.6 with 4, 256 short histories 238, 240 and 241, 64
+// rows of 256 dims 92, 91.5 and 90.5; with no such places the ragged batch took
+// half as long again), then its steps (cut between any two pages the ragged batch
+// took 3% longer).  A span is at least kLeastSpan places long.
 constexpr int kLeastSpan = 3;
 
 // ---- codes to MFMA operands (exact) --------------------------------------
@@ -136,11 +141,13 @@ struct Dwords {
   uint32_t v[N];
 };
 // `at` is uniform and `lane` the lane's own offset, so that the address takes one register.
-// Non-temporal where 16 lanes read whole 128-byte lines (V up to 128 dims),
-// each once: 256 histories of 1,024 to 4,096 tokens 248 -> 226 us, four of 65,536
-// to 131,072 124 -> 112. Not for the 16-byte pieces, whose lines a later load or
-// another wave reads again: with both non-temporal 233 us for the 256 (109 for the
-// four), and 93 instead of 83 for 64 rows of 256 dims.
+// Non-temporal for V up to 128 dims, whose lines no other wave reads (16 lanes
+// take a row: a whole 128-byte line, or at 64 dims half of one, of which the next
+// load takes the rest): 256 histories of 1,024 to 4,096 tokens 260 -> 238 us, at 64
+// dims 140 -> 137 (but 19.5 -> 20.3 for 32 rows and 64 histories), four of 65,536 to
+// 131,072 134 -> 122. Not for the 16-byte pieces, whose lines a later load or
+// another wave reads again: with both non-temporal 247 us for the 256 (120.5 for
+// the four), and 104 instead of 92 for 64 rows of 256 dims.
 // Pieces of 16 bytes lie `step` bytes apart.
 template <int N>
 __device__ __forceinline__ Dwords<N> load_dwords(const uint8_t* at, uint32_t lane, int step = 16) {
@@ -673,8 +680,8 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
 // attend kernel has, if any: one wave per row.  The parts lie in slots 2w + 1,
 // 2(w + 1), 2(w + 2), ...; lanes take 4 dims each, 64 / (D / 4) parts at a time.
 // (Rows along x: equal histories begin in every n-th workgroup, and along x those
-// would all run on one XCD where n is a multiple of 8; 32 tiles of 64 rows by 256
-// dims in eight parts 8.5 -> 7.0 us.)
+// would all run on one XCD where n is a multiple of 8; the join alone of 32 tiles of
+// 64 rows by 256 dims in eight parts 8.5 -> 7.0 us.)
 template <int D, int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void gqa_join_kernel(GqaAttendLaunch a) {
   const int w = blockIdx.y, lane = threadIdx.x & 63;

@@ -7,7 +7,9 @@
 // heads, and two heads' loads are in flight a lane (four: 68 us instead of 65 for
 // 16,384 tokens of 40 heads by 128).  The angle in turns,
 // position * inv_freq / (2 pi), is formed and reduced to [-1/2, 1/2] in 64 bits:
-// in 32 bits position 2^20 would leave 2^-4 rad of it.
+// in 32 bits position 2^20 would leave 2^-4 rad of it.  What is left of it is
+// rounded to fp32, by 2^-26 of a turn at most, for an fp32 sine and cosine: 2^-22
+// or less of a pair beside the output's 2^-8.
 //
 // Bound: HBM (2 bytes read and 2 written per element); latency for a few tokens.
 #include <hip/hip_runtime.h>
@@ -98,7 +100,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeLaunch p, int32_t he
   }
 }
 
-// Rows of any alignment and any even length, a pair a lane.
+// Rows of any alignment and any even length, a pair a lane, in 2-byte pieces, all
+// of a token's heads on one wave: 92 us for 16,384 tokens of 40 heads by 128 that
+// start at an odd element (68 in 16-byte pieces), 11 for 256 tokens (4.1).
 __global__ __launch_bounds__(kThreads) void rope_any_kernel(RopeLaunch p) {
   __shared__ float cosine[kThreads / 64][kMaxRopePairs], sine[kThreads / 64][kMaxRopePairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
