@@ -57,6 +57,11 @@ constexpr int kWaves = 4;
 constexpr float kPageShift = 15.f;    // a page's weights are 2^(z - peak + 15) against its own largest score
 constexpr float kWeightShift = 6.f;   // sums and outputs are of 2^(z - m + 6)
 constexpr float kMoveAt = 8.f;        // the reference moves once a score passes it by this
+// Scores past this are rounded before the peak is taken off them, as the peak is:
+// in one operation, exactly, against the rounded peak - 15, a weight would be off
+// by what those two roundings leave (at 2^24 powers of two, past fp16's end; up to
+// here 2^-14 at most).
+constexpr float kFar = 1024.f;
 constexpr float kNegInf = -__builtin_inff();
 
 // Places of a tile in the line: kGqaTileCost for its fixed work (two to three
@@ -100,6 +105,12 @@ __device__ __forceinline__ uint32_t pair_to_f16(uint32_t pair) {
     const f16x2 v = __builtin_bit_cast(f16x2, u) - (f16x2){(_Float16)1152.0f, (_Float16)1152.0f};
     return __builtin_bit_cast(uint32_t, v);
   }
+}
+
+// A product rounded by itself, whatever it is added to.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
 }
 
 // What brings a K block's products to base-2 scores: kept off 0 and infinity, so
@@ -192,8 +203,8 @@ struct Shape {
   // of 1,024 to 4,096, 8 rows INT8: 137 us, with one 139 to 140; 64 of 2,048 to
   // 8,192: 16 rows 17.6 and 17.2, 32 rows 20.3 either way).  One for the rest,
   // which two do not hold without scratch or which have half the spans to begin
-  // and join with one: 64 dims E4M3 with 64 rows 27.5 against 31.4 and with 128 rows
-  // 38.5 against 48 (INT8 27.3 either way, 38.7 against 41.6); 128 dims with 16
+  // and join with one: 64 dims E4M3 with 64 rows 27.6 against 31.4 and with 128 rows
+  // 39.4 against 48 (INT8 27.6 either way, 39.7 against 41.6); 128 dims with 16
   // rows and 256 histories 238 against 248; with 32 rows, a ragged batch, 68 against 92.
   static constexpr int kPerCu = D == 64 && MT < 4 ? 2 : 1;
   // the waves' results are joined kPass dims of each share at a time
@@ -542,6 +553,8 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
       // weights (ks brings the products to base-2 scores)
       uint32_t w[MT][S::kTerms][2][4];
       float v_by[MT];  // what brings a row's products to its reference: 2^(peak - m) and V's scale
+      float peaks[MT];  // the rows' largest scores in this page
+      bool far = false;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         float top = kNegInf;
@@ -549,7 +562,22 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
         for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
           for (int i = 0; i < 4; ++i) top = fmaxf(top, z[kt][mt][i]);
-        const float peak = xor_max(top) * ks;  // the row's largest score in this page
+        peaks[mt] = rounded_product(xor_max(top), ks);
+        far |= __builtin_fabsf(peaks[mt]) > kFar && peaks[mt] != kNegInf;
+      }
+      // Far scores by their distances to the peak, each rounded like the peak itself.
+      const bool distances = __any(far);
+      if (distances)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[kt][mt][i] = rounded_product(z[kt][mt][i], ks) - (peaks[mt] == kNegInf ? 0.f : peaks[mt]);
+      const float to_two = distances ? 1.f : ks;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const float peak = peaks[mt];
         if (__any(peak > m[mt] + kMoveAt)) {
           const float now = fmaxf(m[mt], peak);
           const float by = now == kNegInf ? 1.f : __builtin_amdgcn_exp2f(m[mt] - now);
@@ -558,7 +586,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
 #pragma unroll
           for (int j = 0; j < S::kDims; ++j) o[j][mt] *= by;
         }
-        const float ref = peak == kNegInf ? 0.f : peak - kPageShift;
+        const float ref = distances ? -kPageShift : peak == kNegInf ? 0.f : peak - kPageShift;
         const float by = peak == kNegInf ? 0.f : __builtin_amdgcn_exp2f(peak - m[mt] + (kWeightShift - kPageShift));
         float sum = 0.f;
 #pragma unroll
@@ -566,7 +594,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<D, MT, RG>::kPerCu)) void gqa_a
           float e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[kt][mt][i], ks, -ref));
+            e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[kt][mt][i], to_two, -ref));
             sum += e[i];
           }
 #pragma unroll

@@ -99,3 +99,41 @@ def test_attend_of_few_rows_keeps_weights_past_fp16(int8, dim, kv_heads, group):
     err = np.abs(out.float().cpu().numpy().astype(np.float64) - exact)
     assert (2.0 ** -8 * np.abs(exact) < 2.0 ** -13 * mass).any()   # results that cancel are there
     assert np.all(err <= tol), float((err / tol).max())
+
+
+@pytest.mark.parametrize("int8", [False, True], ids=["e4m3", "int8"])
+@pytest.mark.parametrize("power", [8, 10, 18, 24, 27, 30, 40, 60, 100])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("lens,group,q_chunk", [([300, 64, 5], 4, 1), ([9000, 130, 3], 8, 4), ([200, 66], 16, 8)])
+def test_attend_scores_past_fp32s_whole_numbers(int8, power, sign, lens, group, q_chunk):
+    """Scores of +-2^power and more, where neighbouring fp32 values lie far apart: the keys of the largest score share
+    the weight evenly, all others have none; every score positive, or every score negative."""
+    rng = np.random.Generator(np.random.PCG64(70 + power))
+    dim = 64
+    p = Attend(lens, 1, group, dim, q_chunk, int8, seed=71 + power)
+    q = np.zeros((len(lens) * q_chunk, group, dim), dtype=np.float32)
+    q[..., 0] = np.exp2(np.float32(power + 3)) * rng.integers(64, 128, q.shape[:2]).astype(np.float32) / 64   # (bf16 holds these)
+    p.q = f32_to_bf16_bits(q)
+    level = rng.integers(1, 4, p.k.shape[:3])
+    p.k[:] = 0
+    p.k[..., 0] = oracle.step.encode(sign * level.astype(np.float64), int8)
+    p.ks[:] = 1.0
+    out, lse = p.attend()
+    o, l = out.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    V = oracle.step.decode(p.v, int8) * p.vs[..., None, None].astype(np.float64)
+    for b, s in enumerate(lens):
+        at = [(p.table[b, j // PAGE], j % PAGE) for j in range(s)]
+        for i in range(q_chunk):
+            n, row = s - q_chunk + i + 1, b * q_chunk + i
+            if n <= 0:
+                assert np.all(o[row] == 0) and np.all(np.isneginf(l[row]))
+                continue
+            have = np.array([sign * level[page, 0, place] for page, place in at[:n]])
+            vals = np.array([V[page, 0, place] for page, place in at[:n]])[have == have.max()]
+            exact, mass = vals.mean(0), np.abs(vals).mean(0)
+            # bf16's half step, and equal weights: 2^-11 where one fp16 term holds them, and one rounding a key
+            tol = 2.0 ** -8 * np.abs(exact) + (2.0 ** -11 + (n + 64) * 2.0 ** -24) * mass * 1.01
+            assert np.all(np.abs(o[row] - exact) <= tol)
+            z = have.max() * 0.125 * q[row, :, 0].astype(np.float64)
+            # roundings of log2 e, its product with softmax_scale, the block's factor, the score, two sums, ln 2, its product
+            assert np.all(np.abs(l[row] - (z + np.log(len(vals)))) <= 8 * 2.0 ** -24 * np.abs(z) + 2.0 ** -18)
