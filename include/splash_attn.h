@@ -561,6 +561,163 @@ int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, c
                       void* out, float* lse, const splash_gqa_desc* desc, void* workspace, size_t ws_bytes,
                       void* stream);
 
+/*
+ * ---- the latent-attention layer around the cache ----------------------------
+ *
+ * What a layer of a model with one shared latent row a token runs around
+ * splash_mla_attend (App. E: no-position and rotary parts, up-projections), and
+ * in its place for a prompt.  A head's key is [no-position 128 | rotary 64],
+ * its value 128 wide; W_UK[h] and W_UV[h], 128 x 512 each, take the latent to
+ * them.
+ *   decode   splash_mla_absorb_q   q W_UK and the turned rotary part: packed rows
+ *            splash_mla_append     the new tokens' rows into the cache
+ *            splash_mla_attend     (or its shards, or listed positions)
+ *            splash_mla_expand_out latent outputs through W_UV
+ *   prompt   splash_mla_append, splash_mla_gather (histories back as dense rows),
+ *            the caller's product with the up-projections, splash_rope on the
+ *            queries, splash_mla_prefill
+ * Both give the same attention: <q W_UK | q_r, [c | k_r]> = <q, W_UK c> + <q_r, k_r>.
+ *
+ * These calls stay inside their buffers whatever the device data holds, and can
+ * be captured in a graph.  They need no workspace but splash_mla_prefill's.
+ * Strides count elements; `stream` and statuses as above.
+ */
+#define SPLASH_DIM_NOPE   128
+#define SPLASH_DIM_ROPE   64
+#define SPLASH_DIM_VALUE  128
+
+/*
+ * splash_mla_append: the new tokens' rows into the paged cache of any format.
+ *   latent       bf16, element d < 512 of row t at t * latent_stride + d
+ *   key          bf16, element r < 64 of row t at t * key_stride + r: the shared
+ *                rotary key (views of a fused projection's rows)
+ *   norm_weight  bf16 [512], or NULL: the latent is taken as it is
+ *   positions, rope   as for splash_rope with rot_dim 64; rope NULL: the key is
+ *                taken as it is, and positions are not read
+ *   slots        int32 [num_tokens]; row t goes to row slots[t] % 64 of page
+ *                slots[t] / 64; a slot outside [0, 64 * num_pages) is skipped.
+ *                Slots are distinct (two rows of one slot race)
+ *   kv_scales    SPLASH_KV_FP8_E4M3: desc->kv_scales, written; else ignored
+ * With y[0:512] = latent * weight / sqrt(mean(latent^2) + norm_eps), formed in 64
+ * bits and rounded to fp32, and y[512:576] the key's pairs turned (fp32, the angle
+ * in 64 bits):
+ *   SPLASH_KV_BF16        y rounded to bf16
+ *   SPLASH_KV_FP8_E4M3    scale = max|y| / 448 (not below 2^-126; 1 where every y
+ *                         is 0), codes = y / scale, an fp32 quotient, rounded to E4M3
+ *   SPLASH_KV_FP8_LATENT  each 128 latent columns: scale = the least power of two,
+ *                         2^-126 .. 2^63, with max|y| <= 448 * scale (1 where every
+ *                         y is 0), codes = y / scale rounded to E4M3; the key
+ *                         rounded to bf16
+ * all to nearest even.  Maxima are of finite values; infinities (and what lies
+ * past 448 * 2^63) take the largest code of their sign, NaN is E4M3's NaN.
+ * desc: batch (0: a no-op), page_size, num_pages, kv_dtype and kv_scales are
+ * used; num_heads and softmax_scale are only checked; flags are ignored.
+ * Errors: INVALID_ARGUMENT (desc, NULL, num_tokens < 0, negative stride, norm_eps
+ * negative or not finite, kv_scales other than desc's, rope as for splash_rope or
+ * rot_dim != 64), UNSUPPORTED (desc, num_pages or num_tokens past 2^25), MISALIGNED
+ * (latent, key, norm_weight or pages not 16-byte, strides not multiples of 8,
+ * other arrays not 4-byte aligned).
+ */
+int splash_mla_append(const void* latent, int64_t latent_stride, const void* key, int64_t key_stride,
+                      const void* norm_weight, float norm_eps, const int32_t* positions, int64_t position_stride,
+                      const splash_rope_desc* rope, const int32_t* slots, int32_t num_tokens, void* kv_pages,
+                      float* kv_scales, const splash_mla_desc* desc, void* stream);
+
+/*
+ * splash_mla_gather: rows of the cache back as dense bf16.  Rows row_indptr[b] ..
+ * row_indptr[b+1] - 1 of the outputs are the tokens begin_b, begin_b + 1, ... of
+ * request b's history (begin_b = key_begin[b], or 0 where key_begin is NULL):
+ *   row_indptr   int32 [B+1], not decreasing; rows outside [row_indptr[0],
+ *                row_indptr[B]) and past max_rows are left as they are
+ *   latent_out   bf16 [max_rows, 512], row stride latent_stride
+ *   key_out      bf16 [max_rows, 64], row stride key_stride (both may be parts
+ *                of one [max_rows, 576] buffer)
+ * A value is code * scale in fp32, rounded once to bf16 (exact where the scale
+ * is a power of two and the value in bf16's range).  A token outside [0, 64 *
+ * max_pages_per_seq), or whose block-table entry is outside the pool, gives a row of
+ * zeros.  Errors: INVALID_ARGUMENT (desc, NULL, max_rows < 0, strides below the
+ * row), UNSUPPORTED (desc, num_pages or max_rows past 2^25, max_pages_per_seq past
+ * 2^25 - 1), MISALIGNED (pages or outputs not 16-byte, strides not multiples of
+ * 8, other arrays not 4-byte aligned).
+ */
+int splash_mla_gather(const void* kv_pages, const int32_t* block_table, const int32_t* key_begin,
+                      const int32_t* row_indptr, int32_t max_rows, void* latent_out, int64_t latent_stride,
+                      void* key_out, int64_t key_stride, const splash_mla_desc* desc, void* stream);
+
+/*
+ * splash_mla_absorb_q: packed query rows for splash_mla_attend,
+ *   q_out[n,h,0:512] = sum_d q[n,h,d] * w_uk[h,d,:]    (d < 128; fp32 sums)
+ *   q_out[n,h,512:576] = q[n,h,128:192] turned by the token's position (rope NULL:
+ *                        as it is, and positions are not read)
+ * each rounded once to bf16.
+ *   q       bf16, element d < 192 of head h of token n at n * q_token_stride +
+ *           h * q_head_stride + d
+ *   w_uk    bf16, element c < 512 of row d < 128 of head h at h * w_head_stride +
+ *           d * w_row_stride + c (as it stands in a [heads, 256, 512]
+ *           up-projection of keys and values)
+ *   q_out   bf16 [num_tokens, num_heads, 576], over none of the inputs
+ * splash_mla_expand_out: the attention's outputs through the value projection,
+ *   y[n,h,v] = sum_c w_uv[h,v,c] * out[n,h,c]          (c < 512; fp32 sums)
+ *   out     bf16 [num_tokens, num_heads, 512]
+ *   w_uv    bf16, laid out as w_uk: row v < 128 of head h
+ *   y       bf16, element v of head h of token n at n * y_token_stride + h *
+ *           y_head_stride + v; rows must not overlap each other or the inputs
+ * Errors of both: INVALID_ARGUMENT (NULL, negative counts or strides, rows of y
+ * that overlap, rope as for splash_rope or rot_dim != 64), UNSUPPORTED (num_heads
+ * past 1024, num_tokens past 2^24), MISALIGNED (tensors not 16-byte, strides not
+ * multiples of 8, positions not 4-byte aligned).
+ */
+int splash_mla_absorb_q(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* w_uk,
+                        int64_t w_head_stride, int64_t w_row_stride, const int32_t* positions, int64_t position_stride,
+                        const splash_rope_desc* rope, int32_t num_tokens, int32_t num_heads, void* q_out,
+                        void* stream);
+int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stride, int64_t w_row_stride,
+                          int32_t num_tokens, int32_t num_heads, void* y, int64_t y_token_stride, int64_t y_head_stride,
+                          void* stream);
+
+/*
+ * splash_mla_prefill: causal attention of ragged prompts over expanded keys and
+ * values.  Request b's query rows are q_indptr[b] .. q_indptr[b+1] - 1 (nq of
+ * them), its keys the rows kv_indptr[b] .. kv_indptr[b+1] - 1 (nk); query row i
+ * of the request is its token nk - nq + i and sees keys j = 0 .. nk - nq + i (none
+ * where that is negative: out = 0, lse = -inf):
+ *   z_j        = softmax_scale * (<q[n,h,0:128], k[j,h,:]> + <q[n,h,128:192], key[j,:]>)
+ *   lse[n,h]   = ln sum_j exp(z_j)
+ *   out[n,h,:] = sum_j exp(z_j - lse[n,h]) * v[j,h,:]
+ *   q     bf16 [num_rows, num_heads, 192] (rotary part turned), k, v bf16
+ *         [num_keys, num_heads, 128], each with a token and a head stride (k and
+ *         v may be the halves of one [.., 256] projection); key bf16 [num_keys, 64]
+ *         with a token stride
+ *   q_indptr, kv_indptr   int32 [batch+1], not decreasing; what lies past num_rows
+ *         or num_keys is cut off.  Query rows outside [q_indptr[0], q_indptr[batch])
+ *         are left as they are
+ *   out   bf16 [num_rows, num_heads, 128] (round to nearest even)
+ *   lse   fp32 [num_rows, num_heads]; may be NULL
+ *   workspace   splash_mla_prefill_workspace_size bytes, 16-byte aligned; it holds
+ *         what one call leaves for its own second launch, and calls that may overlap
+ *         take one each
+ * Products are summed in fp32; a weight is rounded to bf16 where it meets V (2^-8),
+ * its sum is not.  Keys that a row does not see
+ * do not touch it, whatever they hold (NaN and infinities in k, key and v among
+ * them); a score that is NaN or +inf makes its row NaN.  Deterministic: the same
+ * inputs and sizes give the same bits.
+ * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, softmax_scale not
+ * finite and > 0), UNSUPPORTED (num_heads past 1024, num_rows or num_keys past 2^25,
+ * batch past 2^20, a token stride past 2^24, num_rows * num_heads past 2^31),
+ * MISALIGNED (tensors or workspace not 16-byte, strides not multiples of 8, other
+ * arrays not 4-byte aligned), WORKSPACE_TOO_SMALL.
+ */
+typedef struct splash_mla_rows {
+    const void* x;
+    int64_t token_stride, head_stride;
+} splash_mla_rows;
+
+size_t splash_mla_prefill_workspace_size(int32_t batch, int32_t num_rows, int32_t num_heads);
+int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const void* key, int64_t key_stride,
+                       const splash_mla_rows* v, const int32_t* q_indptr, const int32_t* kv_indptr, int32_t batch,
+                       int32_t num_rows, int32_t num_keys, int32_t num_heads, float softmax_scale, void* out, float* lse,
+                       void* workspace, size_t ws_bytes, void* stream);
+
 /* Number of work units the workspace reserves: B*q_chunk + max_partials. */
 int32_t splash_mla_max_units(int32_t batch, int32_t q_chunk, int32_t max_partials);
 

@@ -21,12 +21,12 @@ torch's float64 scaled-dot-product attention, closed forms, invariants, a
 hand-worked example, and the format definitions cross-checked with numpy and
 torch dtypes).
 """
-from . import dop, step
+from . import dop, layer, step
 from .formats import DS_ROW_BYTES, bf16_bits_to_f64, ds_rows_to_f64, e4m3_bits_to_f64
 from .mla import (gather_history, mla_attention, mla_attention_sampled,
                   merge_partials, attention_rows, gather_positions, mla_attention_topk)
 
-__all__ = ["dop", "step", "bf16_bits_to_f64", "e4m3_bits_to_f64", "ds_rows_to_f64", "DS_ROW_BYTES", "gather_history", "gather_positions",
+__all__ = ["dop", "layer", "step", "bf16_bits_to_f64", "e4m3_bits_to_f64", "ds_rows_to_f64", "DS_ROW_BYTES", "gather_history", "gather_positions",
            "mla_attention_topk",
            "mla_attention", "mla_attention_sampled", "merge_partials",
            "attention_rows"]

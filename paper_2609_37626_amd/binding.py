@@ -95,6 +95,14 @@ class RopeDesc(ctypes.Structure):
     ]
 
 
+class MlaRows(ctypes.Structure):
+    _fields_ = [
+        ("x", ctypes.c_void_p),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
 _lib = None
 
 _VP = ctypes.c_void_p
@@ -133,6 +141,14 @@ _SIGNATURES = {
     "splash_gqa_append": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _I32, _VP, _VP, _VP, _VP, _PG, _VP]),
     "splash_gqa_workspace_size": (_SZ, [_PG, _I32]),
     "splash_gqa_attend": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _VP, _VP, _PG, _VP, _SZ, _VP]),
+    "splash_mla_append": (ctypes.c_int, [_VP, _I64, _VP, _I64, _VP, ctypes.c_float, _VP, _I64, _VP, _VP, _I32, _VP, _VP, _PD,
+                                         _VP]),
+    "splash_mla_gather": (ctypes.c_int, [_VP, _VP, _VP, _VP, _I32, _VP, _I64, _VP, _I64, _PD, _VP]),
+    "splash_mla_absorb_q": (ctypes.c_int, [_VP, _I64, _I64, _VP, _I64, _I64, _VP, _I64, _VP, _I32, _I32, _VP, _VP]),
+    "splash_mla_expand_out": (ctypes.c_int, [_VP, _VP, _I64, _I64, _I32, _I32, _VP, _I64, _I64, _VP]),
+    "splash_mla_prefill_workspace_size": (_SZ, [_I32, _I32, _I32]),
+    "splash_mla_prefill": (ctypes.c_int, [_VP, _VP, _VP, _I64, _VP, _VP, _VP, _I32, _I32, _I32, _I32, ctypes.c_float, _VP, _VP,
+                                          _VP, _SZ, _VP]),
     "splash_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "splash_last_error": (ctypes.c_char_p, []),
     "splash_version": (ctypes.c_char_p, []),
@@ -364,6 +380,7 @@ def _refuse(message: str):
 _I32T = _F32T = _BF16T = None  # torch's types, and the calls that name the device and its current stream (set by _types)
 _device = _raw_stream = None
 _CODES = {}  # code_type: the types of its pages
+_ROWS = {}   # kv_dtype: the types of its pool, and a row's elements
 
 
 def _types():
@@ -371,6 +388,8 @@ def _types():
     import torch
     _I32T, _F32T, _BF16T = torch.int32, torch.float32, torch.bfloat16
     _CODES.update({GQA_E4M3: (torch.uint8, torch.float8_e4m3fn), GQA_INT8: (torch.int8,)})
+    _ROWS.update({KV_BF16: ((torch.bfloat16,), 576), KV_FP8_E4M3: ((torch.uint8, torch.float8_e4m3fn), 576),
+                  KV_FP8_LATENT: ((torch.uint8,), 656)})
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: _current_stream())
     _device = torch._C._cuda_getDevice  # (the calls look at this one: last, for their first use from several threads)
 
@@ -578,6 +597,163 @@ def splash_gqa_attend(q, k_pages, v_pages, k_scales, v_scales, block_table, seq_
         q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
         block_table.data_ptr(), seq_lens.data_ptr(), q_chunk, out.data_ptr(), None if lse is None else lse.data_ptr(), desc,
         workspace.data_ptr(), workspace.numel()), stream)
+
+
+# ------------------------------ the latent-attention layer around the cache
+
+def _pool_ok(desc: MlaDesc, dev: int, kv_pages) -> bool:
+    types, width = _ROWS.get(desc.kv_dtype, ((), 0))
+    return (kv_pages.dtype in types and kv_pages.shape == (desc.num_pages, 64, width) and kv_pages.is_contiguous()
+            and 0 <= dev == kv_pages.get_device())
+
+
+def _refuse_pool(desc: MlaDesc, dev: int, kv_pages, **tensors):
+    types, width = _ROWS.get(desc.kv_dtype, ((), 0))
+    if not types:
+        _refuse(f"unknown kv_dtype {desc.kv_dtype}")
+    _refuse_tensors(dev, kv_pages=(kv_pages, types, (desc.num_pages, 64, width)), **tensors)
+
+
+def _turn_args(positions, rope, tokens: int, dev: int) -> tuple:
+    """(positions, stride, rope) as the C side takes them; rope None: rows are taken as they are."""
+    if rope is None:
+        return None, 0, None
+    if positions is None:
+        _refuse("a rope needs positions")
+    shape, strides = positions.shape, positions.stride()
+    if not (positions.dtype is _I32T and positions.get_device() == dev and len(shape) in (1, 2) and shape[-1] == tokens
+            and (1 if len(shape) == 1 else shape[0]) == rope.num_axes and (tokens < 2 or strides[-1] == 1)):
+        _refuse(f"positions must be int32 [{rope.num_axes}, {tokens}] on the tensors' device, dense along the tokens "
+                f"(got {positions.dtype}, {tuple(shape)}, strides {strides})")
+    return positions.data_ptr(), strides[0] if len(shape) == 2 and shape[0] > 1 else tokens, rope
+
+
+def _refuse_view(name: str, t, shape, dev: int):
+    _refuse(f"{name} must be bf16 {list(shape)} on the GPU, the last dimension dense (got {t.dtype}, {tuple(t.shape)}, "
+            f"strides {t.stride()}, device {t.device})")
+
+
+def _view(name: str, t, shape, dev: int) -> tuple:
+    """The strides of a bf16 view of this shape whose last dimension is dense."""
+    strides = t.stride()
+    if not (t.dtype is _BF16T and t.shape == shape and strides[-1] == 1 and 0 <= dev == t.get_device()):
+        _refuse_view(name, t, shape, dev)
+    return strides
+
+
+def splash_mla_append(latent, key, slots, kv_pages, kv_scales, desc: MlaDesc, norm_weight=None, norm_eps: float = 1e-6,
+                      positions=None, rope: Optional[RopeDesc] = None, stream=None) -> None:
+    """Row t of latent [rows, 512] and key [rows, 64] (views of any row stride) to slot slots[t] of the pool, normed where
+    there is a norm_weight [512], its key turned where there is a rope.  kv_scales: desc's (per-token fp8), else None."""
+    if _device is None:
+        _types()
+    n, dev = slots.numel(), slots.get_device()
+    fp8 = desc.kv_dtype == KV_FP8_E4M3
+    if not (_pool_ok(desc, dev, kv_pages) and slots.dtype is _I32T and slots.is_contiguous()
+            and (norm_weight is None or (norm_weight.dtype is _BF16T and norm_weight.shape == (512,) and norm_weight.is_contiguous()
+                                         and dev == norm_weight.get_device()))
+            and (not fp8 or (kv_scales is not None and kv_scales.dtype is _F32T and kv_scales.shape == (desc.num_pages, 64)
+                             and kv_scales.is_contiguous() and dev == kv_scales.get_device()))):
+        if fp8 and kv_scales is None:
+            _refuse("a per-token fp8 cache needs kv_scales")
+        _refuse_pool(desc, dev, kv_pages, slots=(slots, (_I32T,), (n,)), norm_weight=(norm_weight, (_BF16T,), (512,)),
+                     kv_scales=(kv_scales if fp8 else None, (_F32T,), (desc.num_pages, 64)))
+    at, stride, turn = _turn_args(positions, rope, n, dev)
+    _on_device(dev, lib().splash_mla_append, (
+        latent.data_ptr(), _view("latent", latent, (n, 512), dev)[0], key.data_ptr(), _view("key", key, (n, 64), dev)[0],
+        None if norm_weight is None else norm_weight.data_ptr(), norm_eps, at, stride,
+        None if turn is None else ctypes.byref(turn), slots.data_ptr(), n, kv_pages.data_ptr(),
+        kv_scales.data_ptr() if fp8 else None, desc), stream)
+
+
+def splash_mla_gather(kv_pages, block_table, row_indptr, latent_out, key_out, desc: MlaDesc, key_begin=None,
+                      stream=None) -> None:
+    """Rows row_indptr[b] .. row_indptr[b + 1] - 1 of latent_out [rows, 512] and key_out [rows, 64] (views of any row
+    stride): request b's tokens from key_begin[b] (0) on."""
+    if _device is None:
+        _types()
+    b, rows, dev = desc.batch, latent_out.shape[0], row_indptr.get_device()
+    begin = row_indptr if key_begin is None else key_begin
+    table = (b, desc.max_pages_per_seq)
+    if not (_pool_ok(desc, dev, kv_pages) and block_table.dtype is _I32T and block_table.shape == table
+            and row_indptr.dtype is _I32T and row_indptr.shape == (b + 1,) and begin.dtype is _I32T
+            and (key_begin is None or begin.shape == (b,)) and block_table.is_contiguous() and row_indptr.is_contiguous()
+            and begin.is_contiguous() and dev == block_table.get_device() == begin.get_device()):
+        i32 = (_I32T,)
+        _refuse_pool(desc, dev, kv_pages, block_table=(block_table, i32, table), row_indptr=(row_indptr, i32, (b + 1,)),
+                     key_begin=(key_begin, i32, (b,)))
+    # (one row: its stride may be anything)
+    strides = [_view(name, t, (rows, width), dev)[0] if rows > 1 else _view(name, t, (rows, width), dev) and width
+               for name, t, width in (("latent_out", latent_out, 512), ("key_out", key_out, 64))]
+    _on_device(dev, lib().splash_mla_gather, (
+        kv_pages.data_ptr(), block_table.data_ptr(), None if key_begin is None else key_begin.data_ptr(),
+        row_indptr.data_ptr(), rows, latent_out.data_ptr(), strides[0], key_out.data_ptr(), strides[1], desc), stream)
+
+
+def splash_mla_absorb_q(q, w_uk, q_out, positions=None, rope: Optional[RopeDesc] = None, stream=None) -> None:
+    """q [tokens, heads, 192] (a view of any token and head stride) through w_uk [heads, 128, 512] (any head and row
+    stride), its rotary part turned where there is a rope, into q_out [tokens, heads, 576]."""
+    if _device is None:
+        _types()
+    dev, shape = q.get_device(), q.shape
+    n, h = shape[:2] if len(shape) == 3 else (0, 0)
+    qs, ws = _view("q", q, (n, h, 192), dev), _view("w_uk", w_uk, (h, 128, 512), dev)
+    if _view("q_out", q_out, (n, h, 576), dev) and not q_out.is_contiguous():
+        _refuse("q_out must be contiguous")
+    at, stride, turn = _turn_args(positions, rope, n, dev)
+    _on_device(dev, lib().splash_mla_absorb_q, (
+        q.data_ptr(), qs[0], qs[1], w_uk.data_ptr(), ws[0], ws[1], at, stride, None if turn is None else ctypes.byref(turn),
+        n, h, q_out.data_ptr()), stream)
+
+
+def splash_mla_expand_out(out, w_uv, y, stream=None) -> None:
+    """out [tokens, heads, 512] through w_uv [heads, 128, 512] (any head and row stride) into y [tokens, heads, 128] (any
+    token and head stride)."""
+    if _device is None:
+        _types()
+    dev, shape = out.get_device(), out.shape
+    n, h = shape[:2] if len(shape) == 3 else (0, 0)
+    if _view("out", out, (n, h, 512), dev) and not out.is_contiguous():
+        _refuse("out must be contiguous")
+    ws, ys = _view("w_uv", w_uv, (h, 128, 512), dev), _view("y", y, (n, h, 128), dev)
+    _on_device(dev, lib().splash_mla_expand_out, (
+        out.data_ptr(), w_uv.data_ptr(), ws[0], ws[1], n, h, y.data_ptr(), ys[0], ys[1]), stream)
+
+
+def mla_prefill_workspace_size(batch: int, num_rows: int, num_heads: int) -> int:
+    n = int(lib().splash_mla_prefill_workspace_size(batch, num_rows, num_heads))
+    if n == 0:
+        _refuse("batch, num_rows and num_heads must be >= 0")
+    return n
+
+
+_pack_rows = struct.Struct("@Pqq").pack
+
+
+def splash_mla_prefill(q, k, key, v, q_indptr, kv_indptr, out, lse, workspace, softmax_scale: float = 1.0 / 192 ** 0.5,
+                       stream=None) -> None:
+    """q [rows, heads, 192], k and v [keys, heads, 128], key [keys, 64] (views of any token and head stride) to out
+    [rows, heads, 128] and lse [rows, heads] (may be None)."""
+    if _device is None:
+        _types()
+    dev, shape, keys, b = q.get_device(), q.shape, key.shape[0], q_indptr.numel() - 1
+    n, h = shape[:2] if len(shape) == 3 else (0, 0)
+    qs, ks, vs = (_view(name, t, s, dev) for name, t, s in
+                  (("q", q, (n, h, 192)), ("k", k, (keys, h, 128)), ("v", v, (keys, h, 128))))
+    key_stride = _view("key", key, (keys, 64), dev)[0]
+    if not (out.dtype is _BF16T and out.shape == (n, h, 128) and q_indptr.dtype is _I32T and kv_indptr.dtype is _I32T
+            and b >= 0 and kv_indptr.numel() == b + 1 and workspace.element_size() == 1
+            and (lse is None or (lse.dtype is _F32T and lse.shape == (n, h) and lse.is_contiguous() and lse.get_device() == dev))
+            and out.is_contiguous() and q_indptr.is_contiguous() and kv_indptr.is_contiguous() and workspace.is_contiguous()
+            and dev == out.get_device() == q_indptr.get_device() == kv_indptr.get_device() == workspace.get_device()):
+        import torch
+        i32 = (_I32T,)
+        _refuse_tensors(dev, out=(out, (_BF16T,), (n, h, 128)), lse=(lse, (_F32T,), (n, h)), q_indptr=(q_indptr, i32, None),
+                        kv_indptr=(kv_indptr, i32, (b + 1,)), workspace=(workspace, (torch.uint8, torch.int8), None))
+    _on_device(dev, lib().splash_mla_prefill, (
+        _pack_rows(q.data_ptr(), qs[0], qs[1]), _pack_rows(k.data_ptr(), ks[0], ks[1]), key.data_ptr(), key_stride,
+        _pack_rows(v.data_ptr(), vs[0], vs[1]), q_indptr.data_ptr(), kv_indptr.data_ptr(), b, n, keys, h, softmax_scale,
+        out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel()), stream)
 
 
 def version() -> str:

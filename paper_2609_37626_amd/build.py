@@ -17,7 +17,8 @@ LIB = os.path.join(HERE, "libsplash_attn.so")
 SOURCES = ["attend_bf16.hip", "attend_fp8.hip", "attend_latent.hip", "attend_bf16_topk.hip", "attend_fp8_topk.hip",
            "attend_latent_topk.hip", "attend_exact_fp8.hip", "attend_exact_fp8_topk.hip", "attend_exact_latent.hip",
            "attend_exact_latent_topk.hip", "kernels.hip", "api.cpp", "dop.hip",
-           "step_tables.hip", "rope.hip", "gqa_append.hip", "gqa_attend_e4m3.hip", "gqa_attend_int8.hip", "step_api.cpp"]
+           "step_tables.hip", "rope.hip", "gqa_append.hip", "gqa_attend_e4m3.hip", "gqa_attend_int8.hip", "step_api.cpp",
+           "mla_append.hip", "mla_gather.hip", "mla_project.hip", "mla_prefill.hip", "layer_api.cpp"]
 # measurement helpers for the benchmark, a library of their own
 CALIB_LIB = os.path.join(HERE, "libsplash_calib.so")
 CALIB_SOURCES = ["calib.hip"]

@@ -43,6 +43,30 @@ int hip_fail(hipError_t e, const char* what) {
   return fail(SPLASH_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+int validate_mla_desc(const splash_mla_desc* d, int32_t q_chunk) {
+  if (!d) return fail(SPLASH_ERR_INVALID_ARGUMENT, "desc is NULL");
+  if (d->batch < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "batch < 0");
+  if (q_chunk < 1) return fail(SPLASH_ERR_INVALID_ARGUMENT, "q_chunk must be >= 1 (got %d)", q_chunk);
+  if (d->dim_qk != kDimQK || d->dim_v != kDimV)
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "dims must be qk=576, v=512 (got %d, %d)", d->dim_qk, d->dim_v);
+  if (d->page_size != kPage) return fail(SPLASH_ERR_UNSUPPORTED, "page_size must be 64 (got %d)", d->page_size);
+  if (d->num_heads < 16 || d->num_heads > kMaxHeads || d->num_heads % 16)
+    return fail(SPLASH_ERR_UNSUPPORTED, "num_heads must be a multiple of 16 in [16,128] (got %d)", d->num_heads);
+  if (d->kv_dtype != SPLASH_KV_BF16 && d->kv_dtype != SPLASH_KV_FP8_E4M3 && d->kv_dtype != SPLASH_KV_FP8_LATENT)
+    return fail(SPLASH_ERR_UNSUPPORTED, "unknown kv_dtype %d", d->kv_dtype);
+  if (d->kv_dtype == SPLASH_KV_FP8_E4M3 && !d->kv_scales)
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "fp8 cache needs kv_scales");
+  if (!(std::isfinite(d->softmax_scale) && d->softmax_scale > 0.f))
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
+  if (d->max_pages_per_seq < 1 || d->num_pages < 1)
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "max_pages_per_seq and num_pages must be >= 1");
+  if ((d->flags & SPLASH_FLAG_FORCE_SPLIT) && d->split_pages < 1)
+    return fail(SPLASH_ERR_INVALID_ARGUMENT, "FORCE_SPLIT needs split_pages >= 1");
+  if ((int64_t)d->batch * q_chunk > INT32_MAX / 2)
+    return fail(SPLASH_ERR_UNSUPPORTED, "batch * q_chunk too large");
+  return SPLASH_OK;
+}
+
 }  // namespace splash
 
 namespace {
@@ -104,30 +128,6 @@ Workspace workspace_view(void* ws, int64_t T, int32_t H, int64_t max_partials) {
 int64_t forced_partials(int64_t T, int32_t max_pages_per_seq) {
   if (max_pages_per_seq <= kMaxUnitPages) return 0;
   return T * (int64_t)ceil_div(max_pages_per_seq, kMaxUnitPages);
-}
-
-int validate_desc(const splash_mla_desc* d, int32_t q_chunk) {
-  if (!d) return fail(SPLASH_ERR_INVALID_ARGUMENT, "desc is NULL");
-  if (d->batch < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "batch < 0");
-  if (q_chunk < 1) return fail(SPLASH_ERR_INVALID_ARGUMENT, "q_chunk must be >= 1 (got %d)", q_chunk);
-  if (d->dim_qk != kDimQK || d->dim_v != kDimV)
-    return fail(SPLASH_ERR_INVALID_ARGUMENT, "dims must be qk=576, v=512 (got %d, %d)", d->dim_qk, d->dim_v);
-  if (d->page_size != kPage) return fail(SPLASH_ERR_UNSUPPORTED, "page_size must be 64 (got %d)", d->page_size);
-  if (d->num_heads < 16 || d->num_heads > kMaxHeads || d->num_heads % 16)
-    return fail(SPLASH_ERR_UNSUPPORTED, "num_heads must be a multiple of 16 in [16,128] (got %d)", d->num_heads);
-  if (d->kv_dtype != SPLASH_KV_BF16 && d->kv_dtype != SPLASH_KV_FP8_E4M3 && d->kv_dtype != SPLASH_KV_FP8_LATENT)
-    return fail(SPLASH_ERR_UNSUPPORTED, "unknown kv_dtype %d", d->kv_dtype);
-  if (d->kv_dtype == SPLASH_KV_FP8_E4M3 && !d->kv_scales)
-    return fail(SPLASH_ERR_INVALID_ARGUMENT, "fp8 cache needs kv_scales");
-  if (!(std::isfinite(d->softmax_scale) && d->softmax_scale > 0.f))
-    return fail(SPLASH_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
-  if (d->max_pages_per_seq < 1 || d->num_pages < 1)
-    return fail(SPLASH_ERR_INVALID_ARGUMENT, "max_pages_per_seq and num_pages must be >= 1");
-  if ((d->flags & SPLASH_FLAG_FORCE_SPLIT) && d->split_pages < 1)
-    return fail(SPLASH_ERR_INVALID_ARGUMENT, "FORCE_SPLIT needs split_pages >= 1");
-  if ((int64_t)d->batch * q_chunk > INT32_MAX / 2)
-    return fail(SPLASH_ERR_UNSUPPORTED, "batch * q_chunk too large");
-  return SPLASH_OK;
 }
 
 std::atomic<int32_t> g_workers[64];
@@ -365,7 +365,7 @@ int32_t splash_device_workers(void) {
 
 int splash_mla_plan(const int32_t* seq_lens, int32_t q_chunk, const splash_mla_desc* desc, void* workspace,
                     size_t ws_bytes, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   Workspace wv;
@@ -376,7 +376,7 @@ int splash_mla_plan(const int32_t* seq_lens, int32_t q_chunk, const splash_mla_d
 int splash_mla_run(const void* q, const void* kv_pages, const int32_t* block_table, const int32_t* seq_lens,
                    int32_t q_chunk, void* out, float* lse, const splash_mla_desc* desc, void* workspace,
                    size_t ws_bytes, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if ((st = check_tensors(q, kv_pages, block_table, out, lse)) != SPLASH_OK) return st;
@@ -391,7 +391,7 @@ int splash_mla_run(const void* q, const void* kv_pages, const int32_t* block_tab
 int splash_mla_attend_units(const void* q, const void* kv_pages, const int32_t* block_table,
                             const int32_t* seq_lens, int32_t q_chunk, void* out, float* lse,
                             const splash_mla_desc* desc, void* workspace, size_t ws_bytes, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if ((st = check_tensors(q, kv_pages, block_table, out, lse)) != SPLASH_OK) return st;
@@ -403,7 +403,7 @@ int splash_mla_attend_units(const void* q, const void* kv_pages, const int32_t* 
 
 int splash_mla_combine_splits(int32_t q_chunk, void* out, float* lse, const splash_mla_desc* desc,
                               void* workspace, size_t ws_bytes, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if (!out) return fail(SPLASH_ERR_INVALID_ARGUMENT, "out is NULL");
@@ -420,7 +420,7 @@ int splash_mla_combine_splits(int32_t q_chunk, void* out, float* lse, const spla
 int splash_mla_attend(const void* q, const void* kv_pages, const int32_t* block_table, const int32_t* seq_lens,
                       int32_t q_chunk, void* out, float* lse, const splash_mla_desc* desc, void* workspace,
                       size_t ws_bytes, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if ((st = check_tensors(q, kv_pages, block_table, out, lse)) != SPLASH_OK) return st;
@@ -436,7 +436,7 @@ int splash_mla_attend(const void* q, const void* kv_pages, const int32_t* block_
 int splash_mla_attend_noalloc(const void* q, const void* kv_pages, const int32_t* block_table,
                               const int32_t* seq_lens, int32_t q_chunk, void* out, float* lse,
                               const splash_mla_desc* desc, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->flags & SPLASH_FLAG_DEBUG_CHECK)
     return fail(SPLASH_ERR_UNSUPPORTED,
@@ -459,7 +459,7 @@ int splash_mla_attend_topk(const void* q, const void* kv_pages, const int32_t* b
                            const int32_t* seq_lens, int32_t q_chunk, const int32_t* topk_idx,
                            const int32_t* topk_count, int32_t topk, void* out, float* lse,
                            const splash_mla_desc* desc, void* workspace, size_t ws_bytes, void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if (!topk_idx || !topk_count) return fail(SPLASH_ERR_INVALID_ARGUMENT, "topk_idx and topk_count must be non-NULL");
@@ -508,7 +508,7 @@ int splash_mla_attend_shard(const void* q, const void* kv_pages, const int32_t* 
                             const int32_t* key_end, int32_t num_shards, int32_t shard, float* part_out,
                             float* part_lse, const splash_mla_desc* desc, void* workspace, size_t ws_bytes,
                             void* stream) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if (!key_begin || !key_end || !part_lse)
@@ -574,7 +574,7 @@ int splash_mla_combine(const float* partials, const float* partial_lse, const in
 
 int splash_mla_debug_gather(const void* kv_pages, const int32_t* block_table, const int32_t* seq_lens,
                             const splash_mla_desc* desc, void* dense_out, void* stream) {
-  int st = validate_desc(desc, 1);
+  int st = validate_mla_desc(desc, 1);
   if (st != SPLASH_OK) return st;
   if (desc->batch == 0) return SPLASH_OK;
   if (!kv_pages || !block_table || !seq_lens || !dense_out)
@@ -591,7 +591,7 @@ int splash_mla_debug_gather(const void* kv_pages, const int32_t* block_table, co
 int splash_mla_plan_host(const int32_t* seq_lens_host, int32_t q_chunk, const splash_mla_desc* desc,
                          int32_t num_workers, int32_t max_partials, int32_t* units_out, int32_t max_units,
                          int32_t* indptr_out, int32_t* stats_out, int32_t* worker_start_out) {
-  int st = validate_desc(desc, q_chunk);
+  int st = validate_mla_desc(desc, q_chunk);
   if (st != SPLASH_OK) return st;
   if (num_workers < 1) return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_workers must be >= 1");
   const int32_t B = desc->batch, T = B * q_chunk;

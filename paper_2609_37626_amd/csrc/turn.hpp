@@ -1,0 +1,30 @@
+// The rotary turn of a 64-dim row, an element a lane (gfx950 device code).
+#pragma once
+
+#include "layer.hpp"
+
+namespace splash {
+
+// Sine and cosine (times the turn's scale) of pair j at token n.  The angle in
+// turns, position * inv_freq / (2 pi), is formed and reduced to [-1/2, 1/2] in 64
+// bits (in 32, position 2^20 would leave 2^-4 rad of it); what is left goes
+// through fp32, 2^-22 or less of a pair.
+__device__ __forceinline__ void pair_turn(const TurnLaunch& t, int64_t n, int j, float& cosine, float& sine) {
+  double turns = (double)t.positions[t.axis[j] * t.position_stride + n] * t.turns[j];
+  turns -= __builtin_rint(turns);
+  float s, c;
+  sincospif(2.f * (float)turns, &s, &c);
+  cosine = c * t.scale;
+  sine = s * t.scale;
+}
+
+// The pair of element `lane`, and of its row's value the turned one: (a, b) ->
+// (a cos - b sin, b cos + a sin) with the pair (2j, 2j + 1) or (j, j + 32).
+__device__ __forceinline__ int pair_of(const TurnLaunch& t, int lane) { return t.interleaved ? lane >> 1 : lane & (kRopePairs - 1); }
+__device__ __forceinline__ float turn_element(const TurnLaunch& t, int lane, float x, float cosine, float sine) {
+  const int apart = t.interleaved ? 1 : kRopePairs;
+  const float other = __shfl_xor(x, apart);
+  return lane & apart ? x * cosine + other * sine : x * cosine - other * sine;
+}
+
+}  // namespace splash
