@@ -70,6 +70,18 @@ int check_projection(int32_t num_tokens, int32_t num_heads, const void* w, int64
   return SPLASH_OK;
 }
 
+struct PrefillLayout {
+  size_t part_ml, part_out, total;  // the joined tiles' records come first
+};
+PrefillLayout prefill_layout() {
+  const size_t slots = 2 * (size_t)kPrefillWorkers * kPrefillRows;
+  PrefillLayout l;
+  l.part_ml = sizeof(int4) * kPrefillWorkers;
+  l.part_out = l.part_ml + slots * 2 * sizeof(float);
+  l.total = l.part_out + slots * kValue * sizeof(float);
+  return l;
+}
+
 }  // namespace
 
 extern "C" {
@@ -193,7 +205,7 @@ int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stri
 
 size_t splash_mla_prefill_workspace_size(int32_t batch, int32_t num_rows, int32_t num_heads) {
   if (batch < 0 || num_rows < 0 || num_heads < 0) return 0;
-  return 256;
+  return prefill_layout().total;
 }
 
 int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const void* key, int64_t key_stride,
@@ -250,7 +262,14 @@ int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const
   a.scale_log2 = softmax_scale * 1.44269504088896340736f;
   a.out = static_cast<uint16_t*>(out);
   a.lse = lse;
-  a.workers = splash_device_workers();
+  char* ws = static_cast<char*>(workspace);
+  const PrefillLayout layout = prefill_layout();
+  a.joined = reinterpret_cast<int4*>(ws);
+  a.part_ml = reinterpret_cast<float*>(ws + layout.part_ml);
+  a.part_out = reinterpret_cast<float*>(ws + layout.part_out);
+  // two workgroups a compute unit
+  const int32_t workers = 2 * splash_device_workers() / 8 * 8;
+  a.workers = workers < 8 ? 8 : workers > kPrefillWorkers ? kPrefillWorkers : workers;
   if (!std::isfinite(a.scale_log2)) return fail(SPLASH_ERR_INVALID_ARGUMENT, "softmax_scale * log2(e) passes fp32");
   const hipError_t e = launch_mla_prefill(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SPLASH_OK : hip_fail(e, "mla prefill launch");
