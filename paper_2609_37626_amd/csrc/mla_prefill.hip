@@ -59,10 +59,12 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_s_barrier();
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
 }
-// 16 bytes a lane from base + offset straight to LDS at `lds` + 16 * lane.  Through asm,
-// so that the compiler does not wait for it at every LDS read; the kernel does.
+// 16 bytes a lane from base + offset + ADD straight to LDS at `lds` + 16 * lane.  Through
+// asm, so that the compiler does not wait for it at every LDS read; the kernel does.  (The
+// instruction's own offset moves the LDS address as well: M0 is set that much lower.)
+template <int ADD>
 __device__ __forceinline__ void load_lds(const void* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_sub_u32 m0, %0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 offset:%3" ::"s"(lds), "v"(offset), "s"(base), "n"(ADD) : "memory", "scc");
 }
 
 // A tile: 128 rows of a request, of the head `h`.
@@ -301,13 +303,35 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_AS uint8_t*)lds + 2048 * wave;
   const int32_t load_row = 16 * wave + (lane >> 3);
   const uint32_t chunk0 = 16 * ((lane & 7) ^ swz(load_row)), chunk1 = 16 * ((lane & 7) ^ swz(load_row + 8));
+  const uint32_t k_off = load_row * (uint32_t)a.k_token * 2 + chunk0, key_off = load_row * (uint32_t)a.key_token * 2 + chunk0;
+  const uint32_t v_off = load_row * (uint32_t)a.v_token * 2 + chunk0, next8 = chunk1 - chunk0;
+  const auto load_rows = [&](const uint8_t* kb, const uint8_t* rb, const uint8_t* vb, int slot) {  // all of them there
+    const uint32_t to = lds0 + slot * kKeyBytes, v_to = lds0 + 2 * kKeyBytes + slot * kValueBytes;
+    load_lds<0>(kb, k_off, to);
+    load_lds<128>(kb, k_off, to + kGroupBytes);
+    load_lds<0>(rb, key_off, to + 2 * kGroupBytes);
+    load_lds<0>(vb, v_off, v_to);
+    load_lds<128>(vb, v_off, v_to + kGroupBytes);
+    kb += 16 * a.k_token;
+    rb += 16 * a.key_token;
+    vb += 16 * a.v_token;
+    load_lds<0>(kb, k_off + next8, to + 1024);
+    load_lds<128>(kb, k_off + next8, to + 1024 + kGroupBytes);
+    load_lds<0>(rb, key_off + next8, to + 1024 + 2 * kGroupBytes);
+    load_lds<0>(vb, v_off + next8, v_to + 1024);
+    load_lds<128>(vb, v_off + next8, v_to + 1024 + kGroupBytes);
+  };
   const auto load_step = [&](int32_t step) {
     const int32_t first = step * kKeys, last = tile.keys - 1 - first;
+    const int32_t v_first = max(first - kHalf, 0), v_last = tile.keys - 1 - v_first, v_skip = first - kHalf - v_first;
     const uint8_t* kb = k_base + (int64_t)first * a.k_token * 2;
     const uint8_t* rb = key_base + (int64_t)first * a.key_token * 2;
-    const int32_t v_first = max(first - kHalf, 0), v_last = tile.keys - 1 - v_first, v_skip = first - kHalf - v_first;
     const uint8_t* vb = v_base + (int64_t)v_first * a.v_token * 2;
-    const uint32_t slot = (step - step0) & 1;
+    const int slot = (step - step0) & 1;
+    if (last >= kKeys - 1 && v_skip == 0) {
+      load_rows(kb, rb, vb, slot);
+      return;
+    }
     const uint32_t to = lds0 + slot * kKeyBytes, v_to = lds0 + 2 * kKeyBytes + slot * kValueBytes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -316,14 +340,14 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
       if (last >= 0) {
         const uint32_t from = min(row, last);
         const uint32_t k_at = from * (uint32_t)a.k_token * 2 + chunk, r_at = from * (uint32_t)a.key_token * 2 + chunk;
-        load_lds(kb, k_at, to + 1024 * i);
-        load_lds(kb, k_at + 128, to + 1024 * i + kGroupBytes);
-        load_lds(rb, r_at, to + 1024 * i + 2 * kGroupBytes);
+        load_lds<0>(kb, k_at, to + 1024 * i);
+        load_lds<128>(kb, k_at, to + 1024 * i + kGroupBytes);
+        load_lds<0>(rb, r_at, to + 1024 * i + 2 * kGroupBytes);
       }
       if (v_last >= 0) {
         const uint32_t v_at = (uint32_t)min(max(row + v_skip, 0), v_last) * (uint32_t)a.v_token * 2 + chunk;
-        load_lds(vb, v_at, v_to + 1024 * i);
-        load_lds(vb, v_at + 128, v_to + 1024 * i + kGroupBytes);
+        load_lds<0>(vb, v_at, v_to + 1024 * i);
+        load_lds<128>(vb, v_at, v_to + 1024 * i + kGroupBytes);
       }
     }
   };
@@ -378,8 +402,7 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
   };
   // Moves the reference of the rows whose scores pass it by 2^kSlack (a row by its
   // own scores alone).
-  const auto move = [&](const Scores& z) {
-    const float m0 = highest(z, 0), m1 = highest(z, 1);
+  const auto move = [&](float m0, float m1) {
     if (!__any(m0 > top[0] + kSlack || m1 > top[1] + kSlack)) return;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -423,35 +446,14 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
   // beside the last one's product.  k_at, v_at: where its keys and the last one's values are.
   const auto turn = [&](int32_t half, int k_at, int v_at, Scores& z, const Scores& last) {
     const bool now = half < mine, before = half > 2 * step0 && half - 1 < mine;  // (uniform in the wave)
-    // Groups of four products with the operands of the next ones and a share of the
-    // softmax beside them; nothing moves from group to group.
     if (now) {
-      bf16x8 kf[2][2];
-      kf[0][0] = key_operand(k_at, 0, 0);
-      kf[0][1] = key_operand(k_at, 0, 1);
-      if (before) {
 #pragma unroll
-        for (int s = 0; s < 6; ++s) {
-          if (s < 5) {
-            kf[(s + 1) & 1][0] = key_operand(k_at, s + 1, 0);
-            kf[(s + 1) & 1][1] = key_operand(k_at, s + 1, 1);
-          }
-          score_dims(kf[s & 1], s, z);
-          weigh_pair(last, s);
-          if (s > 3) weigh_pair(last, s + 2);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < 6; ++s) {
-          if (s < 5) {
-            kf[(s + 1) & 1][0] = key_operand(k_at, s + 1, 0);
-            kf[(s + 1) & 1][1] = key_operand(k_at, s + 1, 1);
-          }
-          score_dims(kf[s & 1], s, z);
-        }
+      for (int s = 0; s < 6; ++s) {
+        const bf16x8 kf[2] = {key_operand(k_at, s, 0), key_operand(k_at, s, 1)};
+        score_dims(kf, s, z);
       }
-    } else if (before) {
+    }
+    if (before) {
 #pragma unroll
       for (int n = 0; n < 8; ++n) weigh_pair(last, n);
     }
@@ -469,19 +471,86 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
       if (half * kHalf <= sees0) product(std::false_type{});
       else product(std::true_type{});
     }
-    if (now) move(z);
-    __builtin_amdgcn_sched_barrier(0);
+    if (now) move(highest(z, 0), highest(z, 1));
   };
 
-  if (step0 < step1) load_step(step0);
+  // The same where every row sees every key and both halves have their part: one run
+  // of matrix instructions with all else between them.
+  const auto full_turn = [&](int k_at, int v_at, Scores& z, const Scores& last) {
+#pragma unroll
+    for (int s = 0; s < 6; ++s) {
+      const bf16x8 kf[2] = {key_operand(k_at, s, 0), key_operand(k_at, s, 1)};
+      score_dims(kf, s, z);
+    }
+#pragma unroll
+    for (int n = 0; n < 8; ++n) weigh_pair(last, n);
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, value_operand(v_at, d));
+#pragma unroll
+      for (int r = 0; r < 2; ++r) o[d][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pf[r]), o[d][r], 0, 0, 0);
+    }
+    const float m0 = highest(z, 0), m1 = highest(z, 1);
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 12; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 3, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x402, 1, 0);
+    }
+    move(m0, m1);
+  };
+
   Scores z0, z1;
-  for (int32_t step = step0; step0 < step1 && step <= step1; ++step) {
+  const auto arrive = [&]() {
     wait_vmcnt<0>();
     lds_barrier();  // this step's rows are there, and nobody reads the last one's
+  };
+  const auto general_step = [&](int32_t step) {
+    arrive();
     if (step < step1) load_step(step + 1);
     const int slot = (step - step0) & 1;
     turn(2 * step, slot * kKeyBytes, slot * kValueBytes, z0, z1);
     turn(2 * step + 1, slot * kKeyBytes + 4096, slot * kValueBytes + 4096, z1, z0);
+  };
+  if (step0 < step1) {
+    load_step(step0);
+    general_step(step0);
+    int32_t step = step0 + 1;
+    // steps that all rows of the tile see, while a whole step follows them
+    const int32_t full = min(min(step1, tile.keys / kKeys) - 1, tile.first_sees / kKeys);
+    const bool idle = row0 >= tile.rows;
+    if (step + 1 < full) {
+      const uint8_t* kb = k_base + (int64_t)(step + 1) * kKeys * 2 * a.k_token;
+      const uint8_t* rb = key_base + (int64_t)(step + 1) * kKeys * 2 * a.key_token;
+      const uint8_t* vb = v_base + ((int64_t)(step + 1) * kKeys - kHalf) * 2 * a.v_token;
+      for (; step + 1 < full; step += 2) {
+        const auto one = [&](auto at) {
+          constexpr int slot = decltype(at)::value;
+          arrive();
+          load_rows(kb, rb, vb, 1 - slot);
+          kb += kKeys * 2 * a.k_token;
+          rb += kKeys * 2 * a.key_token;
+          vb += kKeys * 2 * a.v_token;
+          if (idle) return;  // (uniform in the wave)
+          full_turn(slot * kKeyBytes, slot * kValueBytes, z0, z1);
+          full_turn(slot * kKeyBytes + 4096, slot * kValueBytes + 4096, z1, z0);
+        };
+        one(std::integral_constant<int, 1>{});
+        one(std::integral_constant<int, 0>{});
+      }
+    }
+    for (; step <= step1; ++step) general_step(step);
   }
   if (__any(odd)) {
     const int32_t from = max(sees0 / kHalf * kHalf, step0 * kKeys), to = min(mine * kHalf, tile.keys);
