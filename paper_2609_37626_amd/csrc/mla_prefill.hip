@@ -33,6 +33,7 @@ constexpr int kRows = 128;              // query rows of a tile
 constexpr int kWaveRows = 32;
 constexpr int kKeys = 64;               // keys of a step
 constexpr int kHalf = 32;
+constexpr int kAhead = 4;
 constexpr int kGroupBytes = kKeys * 128;
 constexpr int kKeyBytes = 3 * kGroupBytes;    // a step's keys in LDS
 constexpr int kValueBytes = 2 * kGroupBytes;  // and its values
@@ -474,41 +475,53 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
     if (now) move(highest(z, 0), highest(z, 1));
   };
 
-  // The same where every row sees every key and both halves have their part: one run
-  // of matrix instructions with all else between them.
-  const auto full_turn = [&](int k_at, int v_at, Scores& z, const Scores& last) {
+  // The same where every row sees every key and both halves have their part: 40 matrix
+  // instructions in a row, the softmax dealt out between them, operands read kAhead
+  // instructions' pairs before they are multiplied.  (In this order as written: left to
+  // itself the compiler puts all of one kind together.)
+  bf16x8 kf[12], vf[8];
+  const auto full_turn = [&](int k_at, int v_at, int k_next, Scores& z, const Scores& last, auto first_half) {
+    constexpr bool kFirst = decltype(first_half)::value;
+    float p0 = 0.f, p1 = 0.f, m[2] = {-INFINITY, -INFINITY};
+    // pair n's two exponentials, and what becomes of them
+    const auto part = [&](auto at) {
+      constexpr int n = decltype(at)::value >> 1, r = n >> 2, t = n >> 1 & 1, i = 2 * (n & 1);
+      if constexpr ((decltype(at)::value & 1) == 0) {
+        p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(last[t][r][i], a.scale_log2, -top[r]));
+        p1 = __builtin_fmaf(last[t][r][i + 1], a.scale_log2, -top[r]);
+      } else {
+        p1 = __builtin_amdgcn_exp2f(p1);
+        sum[r] += p0;
+        pf[r][n & 3] = pack_bf16x2(p0, p1);
+        sum[r] += p1;
+      }
+    };
+    if constexpr (kFirst) {
 #pragma unroll
-    for (int s = 0; s < 6; ++s) {
-      const bf16x8 kf[2] = {key_operand(k_at, s, 0), key_operand(k_at, s, 1)};
-      score_dims(kf, s, z);
+      for (int i = 0; i < kAhead; ++i) kf[i] = key_operand(k_at, i >> 1, i & 1);
     }
-#pragma unroll
-    for (int n = 0; n < 8; ++n) weigh_pair(last, n);
-#pragma unroll
-    for (int d = 0; d < 8; ++d) {
-      const bf16x8 vf = __builtin_bit_cast(bf16x8, value_operand(v_at, d));
-#pragma unroll
-      for (int r = 0; r < 2; ++r) o[d][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pf[r]), o[d][r], 0, 0, 0);
-    }
-    const float m0 = highest(z, 0), m1 = highest(z, 1);
-    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-    for (int i = 0; i < 12; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 3, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, 1, 0);
-    }
-    move(m0, m1);
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<24>([&](auto at) {
+      constexpr int i = decltype(at)::value >> 1, r = decltype(at)::value & 1, s = i >> 1, t = i & 1;
+      if constexpr (r == 0) {
+        if constexpr (i + kAhead < 12) kf[i + kAhead] = key_operand(k_at, (i + kAhead) >> 1, (i + kAhead) & 1);
+        else vf[i + kAhead - 12] = __builtin_bit_cast(bf16x8, value_operand(v_at, i + kAhead - 12));
+      }
+      z[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[r][s], s == 0 ? (f32x4){0.f, 0.f, 0.f, 0.f} : z[t][r], 0, 0, 0);
+      if constexpr (decltype(at)::value % 3 != 2) part(std::integral_constant<int, decltype(at)::value / 3 * 2 + decltype(at)::value % 3>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    static_for<16>([&](auto at) {
+      constexpr int d = decltype(at)::value >> 1, r = decltype(at)::value & 1;
+      if constexpr (r == 0) {
+        if constexpr (d + kAhead < 8) vf[d + kAhead] = __builtin_bit_cast(bf16x8, value_operand(v_at, d + kAhead));
+        else if constexpr (kFirst) kf[d + kAhead - 8] = key_operand(k_next, (d + kAhead - 8) >> 1, (d + kAhead - 8) & 1);
+      }
+      o[d][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], __builtin_bit_cast(bf16x8, pf[r]), o[d][r], 0, 0, 0);
+      m[d >> 2] = fmaxf(m[d >> 2], z[d >> 1 & 1][d >> 2][2 * (d & 1) + r]);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    move(m[0] * a.scale_log2, m[1] * a.scale_log2);
   };
 
   Scores z0, z1;
@@ -543,8 +556,8 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
           rb += kKeys * 2 * a.key_token;
           vb += kKeys * 2 * a.v_token;
           if (idle) return;  // (uniform in the wave)
-          full_turn(slot * kKeyBytes, slot * kValueBytes, z0, z1);
-          full_turn(slot * kKeyBytes + 4096, slot * kValueBytes + 4096, z1, z0);
+          full_turn(slot * kKeyBytes, slot * kValueBytes, slot * kKeyBytes + 4096, z0, z1, std::true_type{});
+          full_turn(slot * kKeyBytes + 4096, slot * kValueBytes + 4096, 0, z1, z0, std::false_type{});
         };
         one(std::integral_constant<int, 1>{});
         one(std::integral_constant<int, 0>{});
