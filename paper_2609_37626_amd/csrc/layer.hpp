@@ -79,16 +79,17 @@ struct MlaPrefillLaunch {
   float scale_log2;  // softmax_scale * log2(e)
   uint16_t* out;
   float* lse;
-  int32_t workers;   // workgroups that the chip holds, a multiple of 8 of at most kPrefillWorkers
+  int32_t units;     // compute units
+  int32_t workers;   // (made by the launch) workgroups that the chip holds
   // workspace: two partial results per worker, and {first row, rows, head, parts} of
   // the tile that it begins and does not end (first row -1: none)
   int4* joined;      // [workers]
-  float* part_ml;    // [2 workers, 128, 2] reference and sum of a row
-  float* part_out;   // [2 workers, 128, 128]
+  float* part_ml;    // [2 workers, a tile's rows, 2] reference and sum of a row
+  float* part_out;   // [2 workers, a tile's rows, 128]
 };
 
 constexpr int32_t kPrefillWorkers = 512;
-constexpr int32_t kPrefillRows = 128;    // query rows of a tile
+constexpr int32_t kPrefillParts = 512 * 128;  // workers times a tile's rows, at most
 
 hipError_t launch_mla_append(const MlaAppendLaunch& a, hipStream_t s);
 hipError_t launch_mla_gather(const MlaGatherLaunch& a, hipStream_t s);

@@ -74,7 +74,7 @@ struct PrefillLayout {
   size_t part_ml, part_out, total;  // the joined tiles' records come first
 };
 PrefillLayout prefill_layout() {
-  const size_t slots = 2 * (size_t)kPrefillWorkers * kPrefillRows;
+  const size_t slots = 2 * (size_t)kPrefillParts;
   PrefillLayout l;
   l.part_ml = sizeof(int4) * kPrefillWorkers;
   l.part_out = l.part_ml + slots * 2 * sizeof(float);
@@ -267,9 +267,7 @@ int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const
   a.joined = reinterpret_cast<int4*>(ws);
   a.part_ml = reinterpret_cast<float*>(ws + layout.part_ml);
   a.part_out = reinterpret_cast<float*>(ws + layout.part_out);
-  // two workgroups a compute unit
-  const int32_t workers = 2 * splash_device_workers() / 8 * 8;
-  a.workers = workers < 8 ? 8 : workers > kPrefillWorkers ? kPrefillWorkers : workers;
+  a.units = splash_device_workers();
   if (!std::isfinite(a.scale_log2)) return fail(SPLASH_ERR_INVALID_ARGUMENT, "softmax_scale * log2(e) passes fp32");
   const hipError_t e = launch_mla_prefill(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? SPLASH_OK : hip_fail(e, "mla prefill launch");

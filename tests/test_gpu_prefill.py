@@ -48,6 +48,24 @@ def test_few_rows_over_a_long_history(heads):
     check(Prompts([7, 40, 1], [9000, 3001, 6000], heads, seed=5), f"{heads} heads")
 
 
+@pytest.mark.parametrize("new,old,heads", [([800], [0], 80), ([1000, 1100, 7], [0, 30, 0], 40), ([520, 900], [4000, 10], 2),
+                                           ([1, 300, 4096], [0, 0, 0], 24), ([256, 257, 255], [6000, 6000, 6001], 3)])
+def test_tiles_whole_and_cut(new, old, heads):
+    """Long and short tiles in both widths, whole and over several workgroups: some heads against the oracle."""
+    p = Prompts(new, old, heads, seed=sum(new))
+    out, lse = p.run()
+    some = sorted({0, heads // 2, heads - 1})[:3 if max(new) < 2000 else 1]
+    p.q, p.kv, p.heads = p.q[:, some], p.kv[:, some], len(some)
+    assert_prefill(out[:, some], lse[:, some], p.oracle(), int(p.keys.max()), f"{new} over {old}, {heads} heads")
+
+
+def test_more_requests_than_are_ordered():
+    rng = rng_of(16)
+    check(Prompts(rng.integers(0, 3, 300), rng.integers(0, 40, 300), 1, seed=17))
+    p = Prompts([900] + [2] * 299, [100] + [0] * 299, 2, seed=18)
+    check(p, "one long prompt before 299 short ones")
+
+
 def test_rows_that_see_no_key():
     # more query rows than keys: the first ones see none
     check(Prompts([70, 200, 3, 130], [-69, -140, -3, -130], 2, seed=6))
