@@ -664,7 +664,7 @@ int splash_mla_gather(const void* kv_pages, const int32_t* block_table, const in
  *           y_head_stride + v; rows must not overlap each other or the inputs
  * Errors of both: INVALID_ARGUMENT (NULL, negative counts or strides, rows of y
  * that overlap, rope as for splash_rope or rot_dim != 64), UNSUPPORTED (num_heads
- * past 1024, num_tokens past 2^24), MISALIGNED (tensors not 16-byte, strides not
+ * past 1024, num_tokens past 2^24, their product past 2^28), MISALIGNED (tensors not 16-byte, strides not
  * multiples of 8, positions not 4-byte aligned).
  */
 int splash_mla_absorb_q(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* w_uk,
@@ -703,7 +703,8 @@ int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stri
  * inputs and sizes give the same bits.
  * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, softmax_scale not
  * finite and > 0), UNSUPPORTED (num_heads past 1024, num_rows or num_keys past 2^25,
- * batch past 2^20, a token stride past 2^24, num_rows * num_heads past 2^31),
+ * batch past 2^20, a token stride past 2^24, num_rows * num_heads past 2^31 - 1,
+ * (num_rows / 128 + batch) * num_heads past 2^21),
  * MISALIGNED (tensors or workspace not 16-byte, strides not multiples of 8, other
  * arrays not 4-byte aligned), WORKSPACE_TOO_SMALL.
  */

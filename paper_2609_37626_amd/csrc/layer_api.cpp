@@ -21,6 +21,10 @@ constexpr int32_t kMaxPoolPages = 1 << 25;  // a slot (64 * page + place) fits i
 constexpr int32_t kMaxRows = 1 << 25;       // a launch holds less than 2^32 lanes: 64 a row
 constexpr int32_t kMaxProjected = 1 << 24;  // tokens, 16 of them a tile
 constexpr int32_t kMaxLayerHeads = 1024;
+// A launch holds less than 2^32 lanes: at most 8 a row and head of a projection, 512 a
+// tile of 128 rows (and its padding) of a prompt.
+constexpr int64_t kMaxProjectedRows = 1 << 28;
+constexpr int64_t kMaxTiles = 1 << 21;
 constexpr int64_t kMaxTokenStride = 1 << 24;  // 64 rows' byte offsets fit 32 bits
 
 // The pool's limits beyond validate_mla_desc, and its pages.
@@ -63,6 +67,8 @@ int check_projection(int32_t num_tokens, int32_t num_heads, const void* w, int64
   if (num_tokens > kMaxProjected) return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens must be at most 2^24 (got %d)", num_tokens);
   if (num_heads > kMaxLayerHeads)
     return fail(SPLASH_ERR_UNSUPPORTED, "num_heads must be at most %d (got %d)", kMaxLayerHeads, num_heads);
+  if ((int64_t)num_tokens * num_heads > kMaxProjectedRows)
+    return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens * num_heads passes 2^28");
   if (w_head_stride < 0 || w_row_stride < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "negative stride");
   if (!w) return fail(SPLASH_ERR_INVALID_ARGUMENT, "the weight is NULL");
   if (!aligned(w, 16) || w_head_stride % 8 || w_row_stride % 8)
@@ -235,6 +241,8 @@ int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const
     return fail(SPLASH_ERR_UNSUPPORTED, "num_rows and num_keys must be at most 2^25, batch at most 2^20");
   if ((int64_t)num_rows * num_heads > INT32_MAX)
     return fail(SPLASH_ERR_UNSUPPORTED, "num_rows * num_heads passes 2^31 - 1");
+  if ((num_rows / 128 + (int64_t)(batch < num_rows ? batch : num_rows)) * num_heads > kMaxTiles)
+    return fail(SPLASH_ERR_UNSUPPORTED, "(num_rows / 128 + batch) * num_heads passes 2^21");
   if (num_rows == 0 || num_heads == 0 || batch == 0) return SPLASH_OK;
   if (!q->x || !q_indptr || !kv_indptr || !out || !workspace || (num_keys > 0 && (!k->x || !key || !v->x)))
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "NULL buffer");

@@ -22,118 +22,232 @@ namespace splash {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
 constexpr int kTile = 16;      // tokens of a tile
 constexpr int kColumns = 128;  // latent columns of a workgroup of absorb
+constexpr int kHeads = 32;     // heads of a wave of the rotary part
 
 __device__ __forceinline__ bf16x8 load8(const uint16_t* p) { return __builtin_bit_cast(bf16x8, *(const u32x4*)p); }
 __device__ __forceinline__ u32x4 round8(f32x4 lo, f32x4 hi) {
   return (u32x4){pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])};
 }
 
-// Grid: (token chunks, 4 column blocks and the rotary part, heads).
-__global__ __launch_bounds__(kThreads, 2) void mla_absorb_kernel(MlaAbsorbLaunch a, int32_t chunk) {
-  __shared__ __align__(16) uint16_t weight[kNope * kColumns];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, g = lane >> 4;
-  const int64_t begin = (int64_t)blockIdx.x * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
-  const int h = blockIdx.z, block = blockIdx.y;
-  const uint16_t* q = a.q + h * a.q_head;
-  uint16_t* out = a.out + (int64_t)h * kDimQK;
-  const int64_t out_token = (int64_t)a.heads * kDimQK;
+// Workgroups go round the 8 XCDs: `inner` neighbours of one item share one of them, one
+// after the other.  The items' places; false past the last.
+__device__ __forceinline__ bool place(uint32_t at, uint32_t items, uint32_t inner, uint32_t& item, uint32_t& part) {
+  const uint32_t xcd = at & 7, n = at >> 3;
+  part = n % inner;
+  item = n / inner * 8 + xcd;
+  return item < items;
+}
 
-  if (block == kDimV / kColumns) {  // the rotary part, a token a wave
-    for (int64_t n = begin + wave; n < end; n += kThreads / 64) {
-      float x = __builtin_bit_cast(float, (uint32_t)q[n * a.q_token + kNope + lane] << 16);
-      if (a.turn.positions) {
-        float cosine, sine;
-        pair_turn(a.turn, n, pair_of(a.turn, lane), cosine, sine);
-        x = turn_element(a.turn, lane, x, cosine, sine);
+// The rotary part of a token, kHeads heads a wave: the lane's pairs' sines and cosines
+// are made once, 16 bytes of a head a lane.
+__device__ __forceinline__ void turn_heads(const MlaAbsorbLaunch& a, int64_t n, int32_t first, int lane, float (&cosine)[kRopePairs],
+                                           float (&sine)[kRopePairs]) {
+  const uint16_t* q = a.q + n * a.q_token + kNope;
+  uint16_t* out = a.out + n * a.heads * kDimQK + kDimV;
+  const int32_t end = min(first + kHeads, a.heads);
+  const bool turned = a.turn.positions != nullptr;
+  if (turned && lane < kRopePairs) pair_turn(a.turn, n, lane, cosine[lane], sine[lane]);
+  __builtin_amdgcn_wave_barrier();  // (one wave's LDS is in order)
+  if (!turned || a.turn.interleaved) {
+    const int piece = lane & 7;
+    f32x4 c = {1.f, 1.f, 1.f, 1.f}, s = {0.f, 0.f, 0.f, 0.f};
+    if (turned) {
+      c = *(const f32x4*)(cosine + 4 * piece);
+      s = *(const f32x4*)(sine + 4 * piece);
+    }
+    u32x4 x[kHeads / 8];
+#pragma unroll
+    for (int i = 0; i < kHeads / 8; ++i) x[i] = *(const u32x4*)(q + min(first + 8 * i + (lane >> 3), end - 1) * a.q_head + 8 * piece);
+#pragma unroll
+    for (int i = 0; i < kHeads / 8; ++i) {
+      const int32_t h = first + 8 * i + (lane >> 3);
+      if (turned) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x0 = __builtin_bit_cast(float, x[i][j] << 16), x1 = __builtin_bit_cast(float, x[i][j] & 0xffff0000u);
+          x[i][j] = pack_bf16x2(x0 * c[j] - x1 * s[j], x1 * c[j] + x0 * s[j]);
+        }
       }
-      out[n * out_token + kDimV + lane] = (uint16_t)pack_bf16x2(x, 0.f);
+      if (h < end) *(u32x4*)(out + (int64_t)h * kDimQK + 8 * piece) = x[i];
     }
-    return;
-  }
-
-  const uint16_t* w = a.w + h * a.w_head + block * kColumns;
+  } else {
+    const int piece = lane & 3;  // of the first half, and of the second
+    f32x4 c[2], s[2];
 #pragma unroll
-  for (int i = 0; i < kNope * kColumns / 8 / kThreads; ++i) {
-    const int piece = i * kThreads + threadIdx.x, d = piece / (kColumns / 8), at = piece % (kColumns / 8);
-    *(u32x4*)(weight + d * kColumns + 8 * at) = *(const u32x4*)(w + d * a.w_row + 8 * at);
-  }
-  __syncthreads();
-  // A operand of tile 2p + s: row m is column 32 p + 8 (m >> 2) + 4 s + (m & 3); lane (g, c)
-  // takes rows d = 32 k + 8 g .. + 7 of the weight.  A transposing read gives lane c of each
-  // 16 the column c of four rows that the lanes point at, four columns a lane.
-  bf16x8 wf[4][8];
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const uint16_t* at = weight + (32 * k + 8 * g + (c >> 2)) * kColumns + 32 * (t >> 1) + 8 * (c & 3) + 4 * (t & 1);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)at);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)(at + 4 * kColumns));
-      wf[k][t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    for (int k = 0; k < 2; ++k) {
+      c[k] = *(const f32x4*)(cosine + 8 * piece + 4 * k);
+      s[k] = *(const f32x4*)(sine + 8 * piece + 4 * k);
     }
-  for (int64_t n0 = begin + kTile * wave; n0 < end; n0 += kTile * (kThreads / 64)) {
-    const int64_t n = n0 + c;
-    const uint16_t* row = q + min(n, end - 1) * a.q_token + 8 * g;
-    bf16x8 x[4];
+    u32x4 lo[kHeads / 16], hi[kHeads / 16];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = load8(row + 32 * k);
-    f32x4 d[8] = {};
+    for (int i = 0; i < kHeads / 16; ++i) {
+      const uint16_t* x = q + min(first + 16 * i + (lane >> 2), end - 1) * a.q_head + 8 * piece;
+      lo[i] = *(const u32x4*)x;
+      hi[i] = *(const u32x4*)(x + kRopePairs);
+    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int i = 0; i < kHeads / 16; ++i) {
+      const int32_t h = first + 16 * i + (lane >> 2);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) d[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[k][t], x[k], d[t], 0, 0, 0);
-    if (n < end) {
-      uint16_t* to = out + n * out_token + block * kColumns + 8 * g;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) *(u32x4*)(to + 32 * p) = round8(d[2 * p], d[2 * p + 1]);
+      for (int j = 0; j < 4; ++j) {
+        const float c0 = c[j >> 1][2 * (j & 1)], c1 = c[j >> 1][2 * (j & 1) + 1], s0 = s[j >> 1][2 * (j & 1)], s1 = s[j >> 1][2 * (j & 1) + 1];
+        const float a0 = __builtin_bit_cast(float, lo[i][j] << 16), a1 = __builtin_bit_cast(float, lo[i][j] & 0xffff0000u);
+        const float b0 = __builtin_bit_cast(float, hi[i][j] << 16), b1 = __builtin_bit_cast(float, hi[i][j] & 0xffff0000u);
+        lo[i][j] = pack_bf16x2(a0 * c0 - b0 * s0, a1 * c1 - b1 * s1);
+        hi[i][j] = pack_bf16x2(b0 * c0 + a0 * s0, b1 * c1 + a1 * s1);
+      }
+      if (h < end) {
+        uint16_t* to = out + (int64_t)h * kDimQK + 8 * piece;
+        *(u32x4*)to = lo[i];
+        *(u32x4*)(to + kRopePairs) = hi[i];
+      }
     }
   }
 }
 
-// Grid: (token chunks, heads); a wave takes 32 of the head's 128 values.
-__global__ __launch_bounds__(kThreads, 2) void mla_expand_kernel(MlaExpandLaunch a, int32_t chunk) {
+// The first `products` workgroups: a head's block of 128 columns for `chunk` tokens, 32
+// columns a wave; the others: the rotary parts.
+__global__ __launch_bounds__(kThreads, 3) void mla_absorb_kernel(MlaAbsorbLaunch a, int32_t chunk, uint32_t products) {
+  __shared__ __align__(16) uint16_t weight[kNope * kColumns];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x >= products) {
+    float(*trig)[2][kRopePairs] = (float(*)[2][kRopePairs])weight;
+    const int32_t groups = (a.heads + kHeads - 1) / kHeads;
+    const int64_t at = (int64_t)(blockIdx.x - products) * kWaves + wave, n = at / groups;
+    if (n < a.num_tokens) turn_heads(a, n, (int32_t)(at % groups) * kHeads, lane, trig[wave][0], trig[wave][1]);
+    return;
+  }
+  const uint32_t chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
+  uint32_t item, part;
+  if (!place(blockIdx.x, (uint32_t)a.heads * (kDimV / kColumns), chunks, item, part)) return;
+  const int c = lane & 15, g = lane >> 4, h = item / (kDimV / kColumns), block = item % (kDimV / kColumns);
+  const int64_t begin = (int64_t)part * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
+  const uint16_t* q = a.q + h * a.q_head + 8 * g;
+  // two tiles at a time, the next two on their way
+  bf16x8 x[2][2][4];
+  const auto load = [&](int64_t n0, bf16x8 (&to)[2][4]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint16_t* row = q + min(n0 + kTile * t + c, end - 1) * a.q_token;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) to[t][k] = load8(row + 32 * k);
+    }
+  };
+  load(begin, x[0]);
+  const uint16_t* w = a.w + h * a.w_head + block * kColumns;
+  u32x4 piece[kNope * kColumns / 8 / kThreads];
+#pragma unroll
+  for (int i = 0; i < kNope * kColumns / 8 / kThreads; ++i) {
+    const int at = i * kThreads + threadIdx.x;
+    piece[i] = *(const u32x4*)(w + at / (kColumns / 8) * a.w_row + 8 * (at % (kColumns / 8)));
+  }
+#pragma unroll
+  for (int i = 0; i < kNope * kColumns / 8 / kThreads; ++i) *(u32x4*)(weight + 8 * (i * kThreads + threadIdx.x)) = piece[i];
+  __syncthreads();
+  // A operand of tile s: row m is column 32 wave + 8 (m >> 2) + 4 s + (m & 3); lane (g, c)
+  // takes rows d = 32 k + 8 g .. + 7 of the weight.  A transposing read gives lane c of each
+  // 16 the column c of four rows that the lanes point at, four columns a lane.
+  bf16x8 wf[4][2];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint16_t* at = weight + (32 * k + 8 * g + (c >> 2)) * kColumns + 32 * wave + 8 * (c & 3) + 4 * s;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)(at + 4 * kColumns));
+      wf[k][s] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  uint16_t* out = a.out + (int64_t)h * kDimQK + block * kColumns + 32 * wave + 8 * g;
+  const auto multiply = [&](int64_t n0, const bf16x8 (&from)[2][4]) {
+    f32x4 d[2][2] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) d[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[k][s], from[t][k], d[t][s], 0, 0, 0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int64_t n = n0 + kTile * t + c;
+      if (n < end) *(u32x4*)(out + n * a.heads * kDimQK) = round8(d[t][0], d[t][1]);
+    }
+  };
+  for (int64_t n0 = begin; n0 < end; n0 += 4 * kTile) {
+    if (n0 + 2 * kTile < end) load(n0 + 2 * kTile, x[1]);
+    multiply(n0, x[0]);
+    if (n0 + 4 * kTile < end) load(n0 + 4 * kTile, x[0]);
+    if (n0 + 2 * kTile < end) multiply(n0 + 2 * kTile, x[1]);
+  }
+}
+
+// A head for `chunk` tokens.  A wave takes 128 of the 512 latent columns, so that each
+// row is read by one wave once; the four waves' sums meet in LDS, 32 values a wave.
+constexpr int kExpandTiles = 4;                    // tiles of a workgroup, all on their way at once
+constexpr int kSlice = kDimV / kWaves;
+__global__ __launch_bounds__(kThreads, 2) void mla_expand_kernel(MlaExpandLaunch a) {
+  __shared__ __align__(16) float sums[2][kWaves][kTile][kValue + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
-  const int64_t begin = (int64_t)blockIdx.x * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
-  const int h = blockIdx.y;
-  const uint16_t* w = a.w + h * a.w_head + 8 * g;
-  bf16x8 wf[16][2];
+  constexpr int chunk = kTile * kExpandTiles;
+  uint32_t h, part;
+  if (!place(blockIdx.x, a.heads, ((uint32_t)a.num_tokens + chunk - 1) / chunk, h, part)) return;
+  const int64_t begin = (int64_t)part * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
+  const uint16_t* x = a.x + (int64_t)h * kDimV + kSlice * wave + 8 * g;
+  bf16x8 xf[kExpandTiles][4];
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
+  for (int t = 0; t < kExpandTiles; ++t)
+    if (begin + kTile * t < end)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) wf[k][s] = load8(w + (32 * wave + 8 * (c >> 2) + 4 * s + (c & 3)) * a.w_row + 32 * k);
-  const uint16_t* x = a.x + (int64_t)h * kDimV + 8 * g;
-  uint16_t* y = a.y + h * a.y_head + 32 * wave + 8 * g;
-  for (int64_t n0 = begin; n0 < end; n0 += kTile) {
-    const int64_t n = n0 + c;
-    const uint16_t* row = x + min(n, end - 1) * a.heads * kDimV;
-    f32x4 d[2] = {};
+      for (int k = 0; k < 4; ++k) xf[t][k] = load8(x + min(begin + kTile * t + c, end - 1) * a.heads * kDimV + 32 * k);
+  const uint16_t* w = a.w + h * a.w_head + kSlice * wave + 8 * g;
+  bf16x8 wf[8][4];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      const bf16x8 xf = load8(row + 32 * k);
+  for (int v = 0; v < 8; ++v)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) d[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[k][s], xf, d[s], 0, 0, 0);
+    for (int k = 0; k < 4; ++k) wf[v][k] = load8(w + (16 * v + c) * a.w_row + 32 * k);
+#pragma unroll
+  for (int t = 0; t < kExpandTiles; ++t) {
+    const int64_t n0 = begin + kTile * t;
+    if (n0 >= end) break;
+    f32x4 d[8] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int v = 0; v < 8; ++v) d[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[v][k], xf[t][k], d[v], 0, 0, 0);
+    float(*mine)[kValue + 4] = sums[t & 1][wave];  // (two buffers: one barrier a tile)
+#pragma unroll
+    for (int v = 0; v < 8; ++v) *(f32x4*)(&mine[c][16 * v + 4 * g]) = d[v];
+    __syncthreads();
+    // 32 lanes a wave's 32 values of 8 tokens, twice: lane (g, c) values 32 wave + 8 g .. of token c
+    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float* from = &sums[t & 1][i][c][32 * wave + 8 * g];
+      lo += *(const f32x4*)from;
+      hi += *(const f32x4*)(from + 4);
     }
-    if (n < end) *(u32x4*)(y + n * a.y_token) = round8(d[0], d[1]);
+    const int64_t n = n0 + c;
+    if (n < end) *(u32x4*)(a.y + n * a.y_token + h * a.y_head + 32 * wave + 8 * g) = round8(lo, hi);
   }
 }
 
 }  // namespace
 
 hipError_t launch_mla_absorb(const MlaAbsorbLaunch& a, hipStream_t s) {
-  const int32_t chunk = 64;
-  const dim3 grid(((unsigned)a.num_tokens + chunk - 1) / chunk, kDimV / kColumns + 1, (unsigned)a.heads);
-  hipLaunchKernelGGL(mla_absorb_kernel, grid, dim3(kThreads), 0, s, a, chunk);
+  const int32_t chunk = a.num_tokens <= 64 ? 64 : 128;
+  const uint32_t items = (uint32_t)a.heads * (kDimV / kColumns), chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
+  const uint64_t products = (uint64_t)(items + 7) / 8 * 8 * chunks;
+  const uint64_t turns = ((uint64_t)a.num_tokens * ((a.heads + kHeads - 1) / kHeads) + kWaves - 1) / kWaves;
+  hipLaunchKernelGGL(mla_absorb_kernel, dim3((unsigned)(products + turns)), dim3(kThreads), 0, s, a, chunk, (uint32_t)products);
   return hipGetLastError();
 }
 
 hipError_t launch_mla_expand(const MlaExpandLaunch& a, hipStream_t s) {
-  const int32_t chunk = 64;
-  const dim3 grid(((unsigned)a.num_tokens + chunk - 1) / chunk, (unsigned)a.heads);
-  hipLaunchKernelGGL(mla_expand_kernel, grid, dim3(kThreads), 0, s, a, chunk);
+  const uint32_t chunk = kTile * kExpandTiles, chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
+  hipLaunchKernelGGL(mla_expand_kernel, dim3(((uint32_t)a.heads + 7) / 8 * 8 * chunks), dim3(kThreads), 0, s, a);
   return hipGetLastError();
 }
 
