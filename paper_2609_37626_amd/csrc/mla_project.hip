@@ -3,10 +3,12 @@
 //
 // The weight stays: a wave keeps its piece of it in registers as the A operand of
 // v_mfma_f32_16x16x32_bf16 (D^T = W^T X^T) and walks over tiles of 16 tokens, whose
-// rows are the B operand straight from memory (lane (g, c): token c, eight values
-// from 8 g).  D leaves lane (g, c) four rows 4 g .. of token c; a pair of tiles takes
-// the weight's columns in the order that makes them eight neighbouring ones, so that
-// a lane stores 16 bytes and four lanes 64 of a token.
+// rows are the B operand (lane (g, c): token c, eight values from 8 g).  D leaves lane
+// (g, c) four rows 4 g .. of token c; a pair of tiles takes the weight's columns in the
+// order that makes them eight neighbouring ones, so that a lane stores 16 bytes and four
+// lanes 64 of a token.  Operands read from memory as they are multiplied, 64 bytes of each
+// of 16 rows, cost absorb 10 of 23 us (queries) and expand 8 of 17 (the weight) at 256
+// tokens of 128 heads: they come in whole lines straight into LDS instead.
 //
 // Bound: HBM (absorb: 384 bytes read and 1,152 written for 131,072 operations a row
 // and head; expand: 1,024 and 256); for a few tokens the weight, 128 KiB a head.
@@ -15,6 +17,7 @@
 
 #include "device_types.hpp"
 #include "layer.hpp"
+#include "lds_loads.hpp"
 #include "turn.hpp"
 
 namespace splash {
@@ -109,12 +112,16 @@ __device__ __forceinline__ void turn_heads(const MlaAbsorbLaunch& a, int64_t n, 
 }
 
 // The first `products` workgroups: a head's block of 128 columns for `chunk` tokens, 32
-// columns a wave; the others: the rotary parts.
-__global__ __launch_bounds__(kThreads, 3) void mla_absorb_kernel(MlaAbsorbLaunch a, int32_t chunk, uint32_t products) {
-  __shared__ __align__(16) uint16_t weight[kNope * kColumns];
+// columns a wave; the others: the rotary parts.  In LDS the weight and two batches of 64
+// tokens' rows, 256 bytes a row, in chunks of 16 bytes at chunk ^ 4 (row & 3) (the weight:
+// the transposing reads take four rows together) and at chunk ^ (row & 15).
+constexpr int kBatch = 64;
+constexpr int kRowBytes = 2 * kNope;
+__global__ __launch_bounds__(kThreads, 2) void mla_absorb_kernel(MlaAbsorbLaunch a, int32_t chunk, uint32_t products) {
+  __shared__ __align__(16) uint8_t lds[(kNope + 2 * kBatch) * kRowBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (blockIdx.x >= products) {
-    float(*trig)[2][kRopePairs] = (float(*)[2][kRopePairs])weight;
+    float(*trig)[2][kRopePairs] = (float(*)[2][kRopePairs])lds;
     const int32_t groups = (a.heads + kHeads - 1) / kHeads;
     const int64_t at = (int64_t)(blockIdx.x - products) * kWaves + wave, n = at / groups;
     if (n < a.num_tokens) turn_heads(a, n, (int32_t)(at % groups) * kHeads, lane, trig[wave][0], trig[wave][1]);
@@ -125,120 +132,148 @@ __global__ __launch_bounds__(kThreads, 3) void mla_absorb_kernel(MlaAbsorbLaunch
   if (!place(blockIdx.x, (uint32_t)a.heads * (kDimV / kColumns), chunks, item, part)) return;
   const int c = lane & 15, g = lane >> 4, h = item / (kDimV / kColumns), block = item % (kDimV / kColumns);
   const int64_t begin = (int64_t)part * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
-  const uint16_t* q = a.q + h * a.q_head + 8 * g;
-  // two tiles at a time, the next two on their way
-  bf16x8 x[2][2][4];
-  const auto load = [&](int64_t n0, bf16x8 (&to)[2][4]) {
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_AS uint8_t*)lds;
+  const int row = lane >> 4, slot = lane & 15;  // of a load's four rows
+  const uint16_t* w = a.w + h * a.w_head + block * kColumns;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint16_t* row = q + min(n0 + kTile * t + c, end - 1) * a.q_token;
+  for (int i = 0; i < kNope / 4 / kWaves; ++i) {
+    const int d = 4 * (kNope / 4 / kWaves * wave + i) + row;
+    load_lds_from(w + d * a.w_row + 8 * (slot ^ (4 * (d & 3))), lds0 + (d - row) * kRowBytes);
+  }
+  const uint16_t* q = a.q + h * a.q_head;
+  const auto load = [&](int64_t n0) {  // (a row past the last token: that one)
+    const uint32_t to = lds0 + (kNope + ((n0 - begin) & kBatch)) * kRowBytes;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) to[t][k] = load8(row + 32 * k);
+    for (int i = 0; i < kBatch / 4 / kWaves; ++i) {
+      const int t = 4 * (kBatch / 4 / kWaves * wave + i) + row;
+      load_lds_from(q + min(n0 + t, end - 1) * a.q_token + 8 * (slot ^ (t & 15)), to + (t - row) * kRowBytes);
     }
   };
-  load(begin, x[0]);
-  const uint16_t* w = a.w + h * a.w_head + block * kColumns;
-  u32x4 piece[kNope * kColumns / 8 / kThreads];
-#pragma unroll
-  for (int i = 0; i < kNope * kColumns / 8 / kThreads; ++i) {
-    const int at = i * kThreads + threadIdx.x;
-    piece[i] = *(const u32x4*)(w + at / (kColumns / 8) * a.w_row + 8 * (at % (kColumns / 8)));
-  }
-#pragma unroll
-  for (int i = 0; i < kNope * kColumns / 8 / kThreads; ++i) *(u32x4*)(weight + 8 * (i * kThreads + threadIdx.x)) = piece[i];
-  __syncthreads();
+  constexpr int kLoads = kBatch / 4 / kWaves;  // of a batch, by each wave
+  load(begin);
+  load(begin + kBatch);
+  wait_vmcnt<2 * kLoads>();
+  lds_barrier();
   // A operand of tile s: row m is column 32 wave + 8 (m >> 2) + 4 s + (m & 3); lane (g, c)
   // takes rows d = 32 k + 8 g .. + 7 of the weight.  A transposing read gives lane c of each
   // 16 the column c of four rows that the lanes point at, four columns a lane.
+  const LDS_AS uint8_t* buf = (const LDS_AS uint8_t*)lds;
   bf16x8 wf[4][2];
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const uint16_t* at = weight + (32 * k + 8 * g + (c >> 2)) * kColumns + 32 * wave + 8 * (c & 3) + 4 * s;
+      const LDS_AS uint8_t* at = buf + (32 * k + 8 * g + (c >> 2)) * kRowBytes + 16 * ((4 * wave + (c & 3)) ^ (4 * (c >> 2))) + 8 * s;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)at);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)(at + 4 * kColumns));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)(at + 4 * kRowBytes));
       wf[k][s] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
   uint16_t* out = a.out + (int64_t)h * kDimQK + block * kColumns + 32 * wave + 8 * g;
-  const auto multiply = [&](int64_t n0, const bf16x8 (&from)[2][4]) {
-    f32x4 d[2][2] = {};
+  for (int64_t n0 = begin; n0 < end; n0 += kBatch) {
+    wait_vmcnt<kLoads>();  // (loads come in order; the last batch's are younger)
+    lds_barrier();
+    const LDS_AS uint8_t* x = buf + (kNope + ((n0 - begin) & kBatch) + c) * kRowBytes;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int t = 0; t < kBatch / kTile; ++t) {
+      if (n0 + kTile * t >= end) break;
+      f32x4 d[2] = {};
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int k = 0; k < 4; ++k) {
+        const bf16x8 xf = *(const LDS_AS bf16x8*)(x + kTile * kRowBytes * t + 16 * ((4 * k + g) ^ c));
 #pragma unroll
-        for (int s = 0; s < 2; ++s) d[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[k][s], from[t][k], d[t][s], 0, 0, 0);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
+        for (int s = 0; s < 2; ++s) d[s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[k][s], xf, d[s], 0, 0, 0);
+      }
       const int64_t n = n0 + kTile * t + c;
-      if (n < end) *(u32x4*)(out + n * a.heads * kDimQK) = round8(d[t][0], d[t][1]);
+      if (n < end) *(u32x4*)(out + n * a.heads * kDimQK) = round8(d[0], d[1]);
     }
-  };
-  for (int64_t n0 = begin; n0 < end; n0 += 4 * kTile) {
-    if (n0 + 2 * kTile < end) load(n0 + 2 * kTile, x[1]);
-    multiply(n0, x[0]);
-    if (n0 + 4 * kTile < end) load(n0 + 4 * kTile, x[0]);
-    if (n0 + 2 * kTile < end) multiply(n0 + 2 * kTile, x[1]);
+    lds_barrier();  // nobody reads these rows any more
+    load(n0 + 2 * kBatch);  // (past the chunk: its last row, so that every batch counts as many)
   }
+  wait_vmcnt<0>();
 }
 
-// A head for `chunk` tokens.  A wave takes 128 of the 512 latent columns, so that each
-// row is read by one wave once; the four waves' sums meet in LDS, 32 values a wave.
-constexpr int kExpandTiles = 4;                    // tiles of a workgroup, all on their way at once
-constexpr int kSlice = kDimV / kWaves;
-__global__ __launch_bounds__(kThreads, 2) void mla_expand_kernel(MlaExpandLaunch a) {
-  __shared__ __align__(16) float sums[2][kWaves][kTile][kValue + 4];
+// A head for 128 tokens.  Waves w and w + 4 take 128 of the 512 latent columns, 64 tokens
+// each, so that each row is read by one wave once; the four slices' sums meet in LDS, 32
+// values a wave.  The weight comes through LDS in whole lines, 256 bytes of a row to a
+// slice, in chunks of 16 bytes at chunk ^ (row & 15).
+constexpr int kSlices = 4;
+constexpr int kSlice = kDimV / kSlices;
+constexpr int kExpandWaves = 2 * kSlices;
+constexpr int kExpandTiles = 4;  // tiles of a wave, all on their way at once
+constexpr int kExpandChunk = 2 * kTile * kExpandTiles;
+__global__ __launch_bounds__(64 * kExpandWaves, 2) void mla_expand_kernel(MlaExpandLaunch a) {
+  typedef float Sums[kExpandWaves][kTile][kValue + 4];
+  __shared__ __align__(16) uint8_t lds[2 * sizeof(Sums)];
+  static_assert(sizeof(lds) >= kValue * kDimV * 2, "the weight");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, g = lane >> 4;
-  constexpr int chunk = kTile * kExpandTiles;
+  const int c = lane & 15, g = lane >> 4, slice = wave % kSlices, side = wave / kSlices;
   uint32_t h, part;
-  if (!place(blockIdx.x, a.heads, ((uint32_t)a.num_tokens + chunk - 1) / chunk, h, part)) return;
-  const int64_t begin = (int64_t)part * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
-  const uint16_t* x = a.x + (int64_t)h * kDimV + kSlice * wave + 8 * g;
+  if (!place(blockIdx.x, a.heads, ((uint32_t)a.num_tokens + kExpandChunk - 1) / kExpandChunk, h, part)) return;
+  const int64_t first = (int64_t)part * kExpandChunk;
+  const int64_t begin = min(first + side * (kExpandChunk / 2), (int64_t)a.num_tokens);
+  const int64_t end = min(begin + kExpandChunk / 2, (int64_t)a.num_tokens);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_AS uint8_t*)lds;
+  const uint16_t* w = a.w + h * a.w_head + kSlice * slice;
+  const int row = lane >> 4, slot = lane & 15;  // of a load's four rows
+#pragma unroll
+  for (int i = 0; i < kValue / 8; ++i) {
+    const int v = kValue / 2 * side + 4 * i + row;
+    load_lds_from(w + v * a.w_row + 8 * (slot ^ (v & 15)), lds0 + (slice * kValue + v - row) * kRowBytes);
+  }
+  const uint16_t* x = a.x + (int64_t)h * kDimV + kSlice * slice + 8 * g;
   bf16x8 xf[kExpandTiles][4];
 #pragma unroll
   for (int t = 0; t < kExpandTiles; ++t)
     if (begin + kTile * t < end)
 #pragma unroll
       for (int k = 0; k < 4; ++k) xf[t][k] = load8(x + min(begin + kTile * t + c, end - 1) * a.heads * kDimV + 32 * k);
-  const uint16_t* w = a.w + h * a.w_head + kSlice * wave + 8 * g;
+  wait_vmcnt<0>();
+  lds_barrier();
+  const LDS_AS uint8_t* buf = (const LDS_AS uint8_t*)lds + (slice * kValue + c) * kRowBytes;
   bf16x8 wf[8][4];
 #pragma unroll
   for (int v = 0; v < 8; ++v)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) wf[v][k] = load8(w + (16 * v + c) * a.w_row + 32 * k);
+    for (int k = 0; k < 4; ++k) wf[v][k] = *(const LDS_AS bf16x8*)(buf + 16 * kRowBytes * v + 16 * ((4 * k + g) ^ c));
+  lds_barrier();  // the weight's place becomes the sums'
+  Sums* sums = (Sums*)lds;
 #pragma unroll
   for (int t = 0; t < kExpandTiles; ++t) {
+    if (first + kTile * t >= a.num_tokens) break;  // (of the first side: the same for all waves)
     const int64_t n0 = begin + kTile * t;
-    if (n0 >= end) break;
-    f32x4 d[8] = {};
+    if (n0 < end) {
+      f32x4 d[8] = {};
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int v = 0; v < 8; ++v) d[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[v][k], xf[t][k], d[v], 0, 0, 0);
-    float(*mine)[kValue + 4] = sums[t & 1][wave];  // (two buffers: one barrier a tile)
+        for (int v = 0; v < 8; ++v) d[v] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[v][k], xf[t][k], d[v], 0, 0, 0);
 #pragma unroll
-    for (int v = 0; v < 8; ++v) *(f32x4*)(&mine[c][16 * v + 4 * g]) = d[v];
-    __syncthreads();
-    // 32 lanes a wave's 32 values of 8 tokens, twice: lane (g, c) values 32 wave + 8 g .. of token c
-    f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      const float* from = &sums[t & 1][i][c][32 * wave + 8 * g];
-      lo += *(const f32x4*)from;
-      hi += *(const f32x4*)(from + 4);
+      for (int v = 0; v < 8; ++v) *(f32x4*)(&sums[t & 1][wave][c][16 * v + 4 * g]) = d[v];  // (two buffers: one barrier a tile)
     }
+    __syncthreads();
     const int64_t n = n0 + c;
-    if (n < end) *(u32x4*)(a.y + n * a.y_token + h * a.y_head + 32 * wave + 8 * g) = round8(lo, hi);
+    if (n < end) {
+      // lane (g, c): values 32 slice + 8 g .. of token c
+      f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll
+      for (int i = 0; i < kSlices; ++i) {
+        const float* from = &sums[t & 1][kSlices * side + i][c][32 * slice + 8 * g];
+        lo += *(const f32x4*)from;
+        hi += *(const f32x4*)(from + 4);
+      }
+      *(u32x4*)(a.y + n * a.y_token + h * a.y_head + 32 * slice + 8 * g) = round8(lo, hi);
+    }
   }
 }
 
 }  // namespace
 
 hipError_t launch_mla_absorb(const MlaAbsorbLaunch& a, hipStream_t s) {
-  const int32_t chunk = a.num_tokens <= 64 ? 64 : 128;
-  const uint32_t items = (uint32_t)a.heads * (kDimV / kColumns), chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
+  // Tokens of a workgroup: what leaves 512 of them, 64 to 256.
+  const uint32_t items = (uint32_t)a.heads * (kDimV / kColumns);
+  const int64_t each = ((int64_t)a.num_tokens * items / 512 + kBatch - 1) / kBatch * kBatch;
+  const int32_t chunk = each < kBatch ? kBatch : each > 4 * kBatch ? 4 * kBatch : (int32_t)each;
+  const uint32_t chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
   const uint64_t products = (uint64_t)(items + 7) / 8 * 8 * chunks;
   const uint64_t turns = ((uint64_t)a.num_tokens * ((a.heads + kHeads - 1) / kHeads) + kWaves - 1) / kWaves;
   hipLaunchKernelGGL(mla_absorb_kernel, dim3((unsigned)(products + turns)), dim3(kThreads), 0, s, a, chunk, (uint32_t)products);
@@ -246,8 +281,8 @@ hipError_t launch_mla_absorb(const MlaAbsorbLaunch& a, hipStream_t s) {
 }
 
 hipError_t launch_mla_expand(const MlaExpandLaunch& a, hipStream_t s) {
-  const uint32_t chunk = kTile * kExpandTiles, chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
-  hipLaunchKernelGGL(mla_expand_kernel, dim3(((uint32_t)a.heads + 7) / 8 * 8 * chunks), dim3(kThreads), 0, s, a);
+  const uint32_t chunks = ((uint32_t)a.num_tokens + kExpandChunk - 1) / kExpandChunk;
+  hipLaunchKernelGGL(mla_expand_kernel, dim3(((uint32_t)a.heads + 7) / 8 * 8 * chunks), dim3(64 * kExpandWaves), 0, s, a);
   return hipGetLastError();
 }
 
