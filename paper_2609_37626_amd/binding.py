@@ -141,10 +141,11 @@ _SIGNATURES = {
     "splash_gqa_append": (ctypes.c_int, [_VP, _VP, _I64, _I64, _VP, _I32, _VP, _VP, _VP, _VP, _PG, _VP]),
     "splash_gqa_workspace_size": (_SZ, [_PG, _I32]),
     "splash_gqa_attend": (ctypes.c_int, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _I32, _VP, _VP, _PG, _VP, _SZ, _VP]),
-    "splash_mla_append": (ctypes.c_int, [_VP, _I64, _VP, _I64, _VP, ctypes.c_float, _VP, _I64, _VP, _VP, _I32, _VP, _VP, _PD,
-                                         _VP]),
+    "splash_mla_append": (ctypes.c_int, [_VP, _I64, _VP, _I64, _VP, ctypes.c_float, _VP, _I64, ctypes.POINTER(RopeDesc), _VP,
+                                         _I32, _VP, _VP, _PD, _VP]),
     "splash_mla_gather": (ctypes.c_int, [_VP, _VP, _VP, _VP, _I32, _VP, _I64, _VP, _I64, _PD, _VP]),
-    "splash_mla_absorb_q": (ctypes.c_int, [_VP, _I64, _I64, _VP, _I64, _I64, _VP, _I64, _VP, _I32, _I32, _VP, _VP]),
+    "splash_mla_absorb_q": (ctypes.c_int, [_VP, _I64, _I64, _VP, _I64, _I64, _VP, _I64, ctypes.POINTER(RopeDesc), _I32, _I32,
+                                           _VP, _VP]),
     "splash_mla_expand_out": (ctypes.c_int, [_VP, _VP, _I64, _I64, _I32, _I32, _VP, _I64, _I64, _VP]),
     "splash_mla_prefill_workspace_size": (_SZ, [_I32, _I32, _I32]),
     "splash_mla_prefill": (ctypes.c_int, [_VP, _VP, _VP, _I64, _VP, _VP, _VP, _I32, _I32, _I32, _I32, ctypes.c_float, _VP, _VP,
@@ -601,12 +602,6 @@ def splash_gqa_attend(q, k_pages, v_pages, k_scales, v_scales, block_table, seq_
 
 # ------------------------------ the latent-attention layer around the cache
 
-def _pool_ok(desc: MlaDesc, dev: int, kv_pages) -> bool:
-    types, width = _ROWS.get(desc.kv_dtype, ((), 0))
-    return (kv_pages.dtype in types and kv_pages.shape == (desc.num_pages, 64, width) and kv_pages.is_contiguous()
-            and 0 <= dev == kv_pages.get_device())
-
-
 def _refuse_pool(desc: MlaDesc, dev: int, kv_pages, **tensors):
     types, width = _ROWS.get(desc.kv_dtype, ((), 0))
     if not types:
@@ -614,31 +609,27 @@ def _refuse_pool(desc: MlaDesc, dev: int, kv_pages, **tensors):
     _refuse_tensors(dev, kv_pages=(kv_pages, types, (desc.num_pages, 64, width)), **tensors)
 
 
+def _refuse_views(dev: int, **views):
+    """Says which bf16 view is not of its shape, dense along the last dimension and on the device (name=(tensor, shape))."""
+    for name, (t, shape) in views.items():
+        if not (t.dtype is _BF16T and t.shape == tuple(shape) and t.stride()[-1] == 1 and 0 <= dev == t.get_device()):
+            _refuse(f"{name} must be bf16 {list(shape)} on the GPU, the last dimension dense (got {t.dtype}, {tuple(t.shape)}, "
+                    f"strides {t.stride()}, device {t.device})")
+
+
 def _turn_args(positions, rope, tokens: int, dev: int) -> tuple:
-    """(positions, stride, rope) as the C side takes them; rope None: rows are taken as they are."""
-    if rope is None:
-        return None, 0, None
+    """(positions, stride) as the C side takes them."""
     if positions is None:
         _refuse("a rope needs positions")
-    shape, strides = positions.shape, positions.stride()
-    if not (positions.dtype is _I32T and positions.get_device() == dev and len(shape) in (1, 2) and shape[-1] == tokens
-            and (1 if len(shape) == 1 else shape[0]) == rope.num_axes and (tokens < 2 or strides[-1] == 1)):
-        _refuse(f"positions must be int32 [{rope.num_axes}, {tokens}] on the tensors' device, dense along the tokens "
+    shape, strides, axes = positions.shape, positions.stride(), rope.num_axes
+    if not (positions.dtype is _I32T and positions.get_device() == dev and (tokens < 2 or strides[-1] == 1)
+            and (shape == (axes, tokens) or (axes == 1 and shape == (tokens,)))):
+        _refuse(f"positions must be int32 [{axes}, {tokens}] on the tensors' device, dense along the tokens "
                 f"(got {positions.dtype}, {tuple(shape)}, strides {strides})")
-    return positions.data_ptr(), strides[0] if len(shape) == 2 and shape[0] > 1 else tokens, rope
+    return positions.data_ptr(), strides[0] if axes > 1 else tokens
 
 
-def _refuse_view(name: str, t, shape, dev: int):
-    _refuse(f"{name} must be bf16 {list(shape)} on the GPU, the last dimension dense (got {t.dtype}, {tuple(t.shape)}, "
-            f"strides {t.stride()}, device {t.device})")
-
-
-def _view(name: str, t, shape, dev: int) -> tuple:
-    """The strides of a bf16 view of this shape whose last dimension is dense."""
-    strides = t.stride()
-    if not (t.dtype is _BF16T and t.shape == shape and strides[-1] == 1 and 0 <= dev == t.get_device()):
-        _refuse_view(name, t, shape, dev)
-    return strides
+_NO_TURN = (None, 0)
 
 
 def splash_mla_append(latent, key, slots, kv_pages, kv_scales, desc: MlaDesc, norm_weight=None, norm_eps: float = 1e-6,
@@ -647,23 +638,26 @@ def splash_mla_append(latent, key, slots, kv_pages, kv_scales, desc: MlaDesc, no
     there is a norm_weight [512], its key turned where there is a rope.  kv_scales: desc's (per-token fp8), else None."""
     if _device is None:
         _types()
-    n, dev = slots.numel(), slots.get_device()
-    fp8 = desc.kv_dtype == KV_FP8_E4M3
-    if not (_pool_ok(desc, dev, kv_pages) and slots.dtype is _I32T and slots.is_contiguous()
-            and (norm_weight is None or (norm_weight.dtype is _BF16T and norm_weight.shape == (512,) and norm_weight.is_contiguous()
-                                         and dev == norm_weight.get_device()))
-            and (not fp8 or (kv_scales is not None and kv_scales.dtype is _F32T and kv_scales.shape == (desc.num_pages, 64)
+    n, dev, kind, pages = slots.numel(), slots.get_device(), desc.kv_dtype, desc.num_pages
+    types, width = _ROWS.get(kind, ((), 0))
+    fp8, ls, ks = kind == KV_FP8_E4M3, latent.stride(), key.stride()
+    if not (latent.dtype is _BF16T and key.dtype is _BF16T and latent.shape == (n, 512) and key.shape == (n, 64)
+            and ls[1] == 1 == ks[1] and slots.dtype is _I32T and slots.is_contiguous() and kv_pages.dtype in types
+            and kv_pages.shape == (pages, 64, width) and kv_pages.is_contiguous()
+            and 0 <= dev == latent.get_device() == key.get_device() == kv_pages.get_device()
+            and (norm_weight is None or (norm_weight.dtype is _BF16T and norm_weight.shape == (512,)
+                                         and norm_weight.is_contiguous() and dev == norm_weight.get_device()))
+            and (not fp8 or (kv_scales is not None and kv_scales.dtype is _F32T and kv_scales.shape == (pages, 64)
                              and kv_scales.is_contiguous() and dev == kv_scales.get_device()))):
         if fp8 and kv_scales is None:
             _refuse("a per-token fp8 cache needs kv_scales")
+        _refuse_views(dev, latent=(latent, (n, 512)), key=(key, (n, 64)))
         _refuse_pool(desc, dev, kv_pages, slots=(slots, (_I32T,), (n,)), norm_weight=(norm_weight, (_BF16T,), (512,)),
-                     kv_scales=(kv_scales if fp8 else None, (_F32T,), (desc.num_pages, 64)))
-    at, stride, turn = _turn_args(positions, rope, n, dev)
+                     kv_scales=(kv_scales if fp8 else None, (_F32T,), (pages, 64)))
+    at, stride = _NO_TURN if rope is None else _turn_args(positions, rope, n, dev)
     _on_device(dev, lib().splash_mla_append, (
-        latent.data_ptr(), _view("latent", latent, (n, 512), dev)[0], key.data_ptr(), _view("key", key, (n, 64), dev)[0],
-        None if norm_weight is None else norm_weight.data_ptr(), norm_eps, at, stride,
-        None if turn is None else ctypes.byref(turn), slots.data_ptr(), n, kv_pages.data_ptr(),
-        kv_scales.data_ptr() if fp8 else None, desc), stream)
+        latent.data_ptr(), ls[0], key.data_ptr(), ks[0], None if norm_weight is None else norm_weight.data_ptr(), norm_eps,
+        at, stride, rope, slots.data_ptr(), n, kv_pages.data_ptr(), kv_scales.data_ptr() if fp8 else None, desc), stream)
 
 
 def splash_mla_gather(kv_pages, block_table, row_indptr, latent_out, key_out, desc: MlaDesc, key_begin=None,
@@ -674,20 +668,25 @@ def splash_mla_gather(kv_pages, block_table, row_indptr, latent_out, key_out, de
         _types()
     b, rows, dev = desc.batch, latent_out.shape[0], row_indptr.get_device()
     begin = row_indptr if key_begin is None else key_begin
-    table = (b, desc.max_pages_per_seq)
-    if not (_pool_ok(desc, dev, kv_pages) and block_table.dtype is _I32T and block_table.shape == table
-            and row_indptr.dtype is _I32T and row_indptr.shape == (b + 1,) and begin.dtype is _I32T
-            and (key_begin is None or begin.shape == (b,)) and block_table.is_contiguous() and row_indptr.is_contiguous()
-            and begin.is_contiguous() and dev == block_table.get_device() == begin.get_device()):
+    types, width = _ROWS.get(desc.kv_dtype, ((), 0))
+    table, ls, ks = (b, desc.max_pages_per_seq), latent_out.stride(), key_out.stride()
+    if not (latent_out.dtype is _BF16T and key_out.dtype is _BF16T and latent_out.shape == (rows, 512)
+            and key_out.shape == (rows, 64) and ls[1] == 1 == ks[1]
+            and kv_pages.dtype in types and kv_pages.shape == (desc.num_pages, 64, width) and kv_pages.is_contiguous()
+            and block_table.dtype is _I32T and block_table.shape == table and row_indptr.dtype is _I32T
+            and row_indptr.shape == (b + 1,) and begin.dtype is _I32T and (key_begin is None or begin.shape == (b,))
+            and block_table.is_contiguous() and row_indptr.is_contiguous() and begin.is_contiguous()
+            and 0 <= dev == latent_out.get_device() == key_out.get_device() == kv_pages.get_device()
+            == block_table.get_device() == begin.get_device()):
         i32 = (_I32T,)
+        _refuse_views(dev, latent_out=(latent_out, (rows, 512)), key_out=(key_out, (rows, 64)))
         _refuse_pool(desc, dev, kv_pages, block_table=(block_table, i32, table), row_indptr=(row_indptr, i32, (b + 1,)),
                      key_begin=(key_begin, i32, (b,)))
-    # (one row: its stride may be anything)
-    strides = [_view(name, t, (rows, width), dev)[0] if rows > 1 else _view(name, t, (rows, width), dev) and width
-               for name, t, width in (("latent_out", latent_out, 512), ("key_out", key_out, 64))]
+    # (of one row the stride may be anything)
     _on_device(dev, lib().splash_mla_gather, (
         kv_pages.data_ptr(), block_table.data_ptr(), None if key_begin is None else key_begin.data_ptr(),
-        row_indptr.data_ptr(), rows, latent_out.data_ptr(), strides[0], key_out.data_ptr(), strides[1], desc), stream)
+        row_indptr.data_ptr(), rows, latent_out.data_ptr(), ls[0] if rows > 1 else 512, key_out.data_ptr(),
+        ks[0] if rows > 1 else 64, desc), stream)
 
 
 def splash_mla_absorb_q(q, w_uk, q_out, positions=None, rope: Optional[RopeDesc] = None, stream=None) -> None:
@@ -695,15 +694,16 @@ def splash_mla_absorb_q(q, w_uk, q_out, positions=None, rope: Optional[RopeDesc]
     stride), its rotary part turned where there is a rope, into q_out [tokens, heads, 576]."""
     if _device is None:
         _types()
-    dev, shape = q.get_device(), q.shape
+    dev, shape, qs, ws = q.get_device(), q.shape, q.stride(), w_uk.stride()
     n, h = shape[:2] if len(shape) == 3 else (0, 0)
-    qs, ws = _view("q", q, (n, h, 192), dev), _view("w_uk", w_uk, (h, 128, 512), dev)
-    if _view("q_out", q_out, (n, h, 576), dev) and not q_out.is_contiguous():
-        _refuse("q_out must be contiguous")
-    at, stride, turn = _turn_args(positions, rope, n, dev)
+    if not (q.dtype is _BF16T and w_uk.dtype is _BF16T and q_out.dtype is _BF16T and shape == (n, h, 192)
+            and w_uk.shape == (h, 128, 512) and q_out.shape == (n, h, 576) and qs[2] == 1 == ws[2] and q_out.is_contiguous()
+            and 0 <= dev == w_uk.get_device() == q_out.get_device()):
+        _refuse_views(dev, q=(q, (n, h, 192)), w_uk=(w_uk, (h, 128, 512)))
+        _refuse_tensors(dev, q_out=(q_out, (_BF16T,), (n, h, 576)))
+    at, stride = _NO_TURN if rope is None else _turn_args(positions, rope, n, dev)
     _on_device(dev, lib().splash_mla_absorb_q, (
-        q.data_ptr(), qs[0], qs[1], w_uk.data_ptr(), ws[0], ws[1], at, stride, None if turn is None else ctypes.byref(turn),
-        n, h, q_out.data_ptr()), stream)
+        q.data_ptr(), qs[0], qs[1], w_uk.data_ptr(), ws[0], ws[1], at, stride, rope, n, h, q_out.data_ptr()), stream)
 
 
 def splash_mla_expand_out(out, w_uv, y, stream=None) -> None:
@@ -711,11 +711,13 @@ def splash_mla_expand_out(out, w_uv, y, stream=None) -> None:
     token and head stride)."""
     if _device is None:
         _types()
-    dev, shape = out.get_device(), out.shape
+    dev, shape, ws, ys = out.get_device(), out.shape, w_uv.stride(), y.stride()
     n, h = shape[:2] if len(shape) == 3 else (0, 0)
-    if _view("out", out, (n, h, 512), dev) and not out.is_contiguous():
-        _refuse("out must be contiguous")
-    ws, ys = _view("w_uv", w_uv, (h, 128, 512), dev), _view("y", y, (n, h, 128), dev)
+    if not (out.dtype is _BF16T and w_uv.dtype is _BF16T and y.dtype is _BF16T and shape == (n, h, 512)
+            and w_uv.shape == (h, 128, 512) and y.shape == (n, h, 128) and ws[2] == 1 == ys[2] and out.is_contiguous()
+            and 0 <= dev == w_uv.get_device() == y.get_device()):
+        _refuse_views(dev, w_uv=(w_uv, (h, 128, 512)), y=(y, (n, h, 128)))
+        _refuse_tensors(dev, out=(out, (_BF16T,), (n, h, 512)))
     _on_device(dev, lib().splash_mla_expand_out, (
         out.data_ptr(), w_uv.data_ptr(), ws[0], ws[1], n, h, y.data_ptr(), ys[0], ys[1]), stream)
 
@@ -738,20 +740,23 @@ def splash_mla_prefill(q, k, key, v, q_indptr, kv_indptr, out, lse, workspace, s
         _types()
     dev, shape, keys, b = q.get_device(), q.shape, key.shape[0], q_indptr.numel() - 1
     n, h = shape[:2] if len(shape) == 3 else (0, 0)
-    qs, ks, vs = (_view(name, t, s, dev) for name, t, s in
-                  (("q", q, (n, h, 192)), ("k", k, (keys, h, 128)), ("v", v, (keys, h, 128))))
-    key_stride = _view("key", key, (keys, 64), dev)[0]
-    if not (out.dtype is _BF16T and out.shape == (n, h, 128) and q_indptr.dtype is _I32T and kv_indptr.dtype is _I32T
-            and b >= 0 and kv_indptr.numel() == b + 1 and workspace.element_size() == 1
+    qs, ks, vs, rs, kv = q.stride(), k.stride(), v.stride(), key.stride(), (keys, h, 128)
+    if not (q.dtype is _BF16T and k.dtype is _BF16T and v.dtype is _BF16T and key.dtype is _BF16T and out.dtype is _BF16T
+            and shape == (n, h, 192) and k.shape == kv and v.shape == kv and key.shape == (keys, 64)
+            and out.shape == (n, h, 128) and qs[2] == ks[2] == vs[2] == rs[1] == 1
+            and q_indptr.dtype is _I32T and kv_indptr.dtype is _I32T and b >= 0 and kv_indptr.numel() == b + 1
+            and workspace.element_size() == 1
             and (lse is None or (lse.dtype is _F32T and lse.shape == (n, h) and lse.is_contiguous() and lse.get_device() == dev))
             and out.is_contiguous() and q_indptr.is_contiguous() and kv_indptr.is_contiguous() and workspace.is_contiguous()
-            and dev == out.get_device() == q_indptr.get_device() == kv_indptr.get_device() == workspace.get_device()):
+            and 0 <= dev == k.get_device() == v.get_device() == key.get_device() == out.get_device() == q_indptr.get_device()
+            == kv_indptr.get_device() == workspace.get_device()):
         import torch
         i32 = (_I32T,)
+        _refuse_views(dev, q=(q, (n, h, 192)), k=(k, kv), v=(v, kv), key=(key, (keys, 64)))
         _refuse_tensors(dev, out=(out, (_BF16T,), (n, h, 128)), lse=(lse, (_F32T,), (n, h)), q_indptr=(q_indptr, i32, None),
                         kv_indptr=(kv_indptr, i32, (b + 1,)), workspace=(workspace, (torch.uint8, torch.int8), None))
     _on_device(dev, lib().splash_mla_prefill, (
-        _pack_rows(q.data_ptr(), qs[0], qs[1]), _pack_rows(k.data_ptr(), ks[0], ks[1]), key.data_ptr(), key_stride,
+        _pack_rows(q.data_ptr(), qs[0], qs[1]), _pack_rows(k.data_ptr(), ks[0], ks[1]), key.data_ptr(), rs[0],
         _pack_rows(v.data_ptr(), vs[0], vs[1]), q_indptr.data_ptr(), kv_indptr.data_ptr(), b, n, keys, h, softmax_scale,
         out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel()), stream)
 

@@ -5,11 +5,16 @@
 // the key's 64, so that every sine and cosine is made once, each store of the wave
 // is one run of bytes, and maxima and the sum of squares are shuffles.
 //
-// y is formed in 64 bits and rounded to fp32 once (x and the weight are bf16, 64-bit
-// products cost what 32-bit ones do here): a value next to 448 * 2^e then decides a
-// scale the same way for everyone, where fp32 sums would leave it to their order.
+// y is formed in 64 bits and rounded to fp32 once (x and the weight are bf16; 64-bit
+// products go at half the rate of 32-bit ones, and there are 32 a lane): a value next to
+// 448 * 2^e then decides a scale the same way for everyone, where fp32 sums would leave
+// it to their order.
 //
-// Bound: HBM for prompts, latency for a token a request.
+// Bound: the instructions of a token, then HBM: 11.1k tokens into per-token E4M3 take
+// 8.9 us for 19 MB (2.8 us at the rate of reads).  Sums and maxima over lanes by row
+// turns and lane reads rather than shuffles through LDS, 1 / sqrt by two Newton steps,
+// quotients by one inverse and a correction and finite values on a path of their own took
+// it from 11.0 us.  A token for each of 256 requests is launch latency: 3.5 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -25,25 +30,109 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kTop = 448.f;
 
-// A quotient by the scale, for the conversion: past the largest code, that code; NaN stays.
-__device__ __forceinline__ float held(float x) { return x != x ? x : fminf(fmaxf(x, -kTop), kTop); }
+template <bool FINITE>
+__device__ __forceinline__ float held(float x) {  // past the largest code, that code; NaN stays
+  return FINITE || x != x ? x : fminf(fmaxf(x, -kTop), kTop);
+}
+template <bool FINITE>
 __device__ __forceinline__ u32x2 codes_of(const float (&y)[8]) {
   u32x2 r;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(held(y[4 * i]), held(y[4 * i + 1]), 0, false);
-    r[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(held(y[4 * i + 2]), held(y[4 * i + 3]), lo, true);
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(held<FINITE>(y[4 * i]), held<FINITE>(y[4 * i + 1]), 0, false);
+    r[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(held<FINITE>(y[4 * i + 2]), held<FINITE>(y[4 * i + 3]), lo, true);
   }
   return r;
 }
-__device__ __forceinline__ float finite_magnitude(float x) {
-  const float m = fabsf(x);
-  return m <= 3.402823466e38f ? m : 0.f;
+
+// Magnitudes as bits: they order like the numbers, with infinities and NaN above all.
+constexpr uint32_t kInfinite = 0x7f800000u;
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t finite_magnitude(float x) { return magnitude(x) < kInfinite ? magnitude(x) : 0u; }
+
+// The 16 lanes of a row of lanes together, in four turns of the row; then all 64.
+template <int BY>
+__device__ __forceinline__ uint32_t turned(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x120 | BY, 0xf, 0xf, true);
+}
+template <int BY>
+__device__ __forceinline__ double turned(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)turned<BY>((uint32_t)(u >> 32)) << 32 | turned<BY>((uint32_t)u));
+}
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, turned<8>(v));
+  v = max(v, turned<4>(v));
+  v = max(v, turned<2>(v));
+  return max(v, turned<1>(v));
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)lane_of((uint32_t)(u >> 32), lane) << 32 | lane_of((uint32_t)u, lane));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = row_max(v);
+  return max(max(lane_of(v, 0), lane_of(v, 16)), max(lane_of(v, 32), lane_of(v, 48)));
 }
 __device__ __forceinline__ double wave_sum(double v) {
+  v += turned<8>(v);
+  v += turned<4>(v);
+  v += turned<2>(v);
+  v += turned<1>(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+// 1 / sqrt(x): the hardware's 2^-26, then two steps of Newton's method (2^-52).
+__device__ __forceinline__ double inverse_root(double x) {
+  const double r = __builtin_amdgcn_rsq(x), h = 0.5 * x;
+  double s = r * __builtin_fma(-h * r, r, 1.5);
+  s = s * __builtin_fma(-h * s, s, 1.5);
+  return r > 0.0 && r < __builtin_inf() ? s : r;  // (x infinite, zero or NaN: r itself)
+}
+// The quotients by one scale, as a division gives them: the product with its inverse and
+// one correction (below 2^-100 the residual would leave fp32's range: a division).
+struct Quotient {
+  float scale, inverse;
+  bool small;
+  __device__ __forceinline__ float operator()(float y) const {
+    if (small) return y / scale;
+    const float q = y * inverse;
+    return fabsf(q) < 1e30f ? copysignf(__builtin_fmaf(__builtin_fmaf(-q, scale, y), inverse, q), y) : q;
+  }
+};
+
+// A token's row into the pool.  FINITE: no infinity and no NaN among its values.
+template <int FORMAT, bool FINITE>
+__device__ __forceinline__ void write_row(const MlaAppendLaunch& a, int32_t slot, int lane, float (&y)[8], float r, uint32_t top) {
+  if constexpr (!FINITE) {
+    top = 0;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+    for (int i = 0; i < 8; ++i) top = max(top, finite_magnitude(y[i]));
+    if (FORMAT == SPLASH_KV_FP8_E4M3) top = max(top, finite_magnitude(r));
+  }
+  if constexpr (FORMAT == SPLASH_KV_FP8_E4M3) {
+    const float largest = __builtin_bit_cast(float, wave_max(top));
+    const float scale = largest > 0.f ? fmaxf(largest / kTop, 0x1p-126f) : 1.f;
+    const Quotient over = {scale, 1.f / scale, scale < 0x1p-100f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = over(y[i]);
+    uint8_t* row = a.pages + (int64_t)slot * kDimQK;
+    *(u32x2*)(row + 8 * lane) = codes_of<FINITE>(y);
+    row[kDimV + lane] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(held<FINITE>(over(r)), 0.f, 0, false);
+    if (lane == 0) a.scales[slot] = scale;
+  } else {
+    // a quarter's 128 columns are 16 lanes; the least e with top <= 1.75 * 2^(e + 8), by
+    // top's exponent and fraction
+    top = row_max(top);
+    int e = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u);
+    e = top > 0 ? min(max(e, -126), 63) : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_ldexpf(y[i], -e);
+    uint8_t* row = a.pages + (int64_t)slot * kLatentRowBytes;
+    *(u32x2*)(row + 8 * lane) = e < 63 ? codes_of<FINITE>(y) : codes_of<false>(y);
+    if ((lane & 15) == 0) *(uint32_t*)(row + kDimV + (lane >> 2)) = (uint32_t)(e + 127) << 23;
+    *(uint16_t*)(row + kDimV + 16 + 2 * lane) = (uint16_t)pack_bf16x2(r, 0.f);
+  }
 }
 
 template <int FORMAT>
@@ -51,10 +140,10 @@ __global__ __launch_bounds__(kThreads) void mla_append_kernel(MlaAppendLaunch a)
   const int lane = threadIdx.x & 63;
   const int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (n >= a.num_tokens) return;
-  const int32_t slot = a.slots[n];
-  if (slot < 0 || (slot >> 6) >= a.num_pages) return;
+  const int32_t slot = __builtin_amdgcn_readfirstlane(a.slots[n]);
   const u32x4 raw = *(const u32x4*)(a.latent + n * a.latent_stride + 8 * lane);
   const float key = __builtin_bit_cast(float, (uint32_t)a.key[n * a.key_stride + lane] << 16);
+  if (slot < 0 || (slot >> 6) >= a.num_pages) return;
   float x[8], y[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -71,8 +160,8 @@ __global__ __launch_bounds__(kThreads) void mla_append_kernel(MlaAppendLaunch a)
     const u32x4 w = *(const u32x4*)(a.norm_weight + 8 * lane);
     double squares = 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) squares += (double)x[i] * (double)x[i];
-    const double by = 1.0 / __builtin_sqrt(wave_sum(squares) * (1.0 / kDimV) + (double)a.norm_eps);
+    for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)x[i], (double)x[i], squares);
+    const double by = inverse_root(wave_sum(squares) * (1.0 / kDimV) + (double)a.norm_eps);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float wi = __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
@@ -90,36 +179,13 @@ __global__ __launch_bounds__(kThreads) void mla_append_kernel(MlaAppendLaunch a)
     for (int i = 0; i < 4; ++i) q[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
     *(u32x4*)(row + 8 * lane) = q;
     row[kDimV + lane] = (uint16_t)pack_bf16x2(r, 0.f);
-    return;
-  }
-  float top = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, finite_magnitude(y[i]));
-  if constexpr (FORMAT == SPLASH_KV_FP8_E4M3) {
-    top = fmaxf(top, finite_magnitude(r));
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float scale = top > 0.f ? fmaxf(top / kTop, 0x1p-126f) : 1.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = y[i] / scale;
-    uint8_t* row = a.pages + (int64_t)slot * kDimQK;
-    *(u32x2*)(row + 8 * lane) = codes_of(y);
-    row[kDimV + lane] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(held(r / scale), 0.f, 0, false);
-    if (lane == 0) a.scales[slot] = scale;
   } else {
-    // a quarter's 128 columns are 16 lanes
+    uint32_t top = 0;
 #pragma unroll
-    for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-    // the least e with top <= 1.75 * 2^(e + 8): by top's exponent and fraction
-    const uint32_t bits = __builtin_bit_cast(uint32_t, top);
-    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
-    e = top > 0.f ? min(max(e, -126), 63) : 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __builtin_amdgcn_ldexpf(y[i], -e);
-    uint8_t* row = a.pages + (int64_t)slot * kLatentRowBytes;
-    *(u32x2*)(row + 8 * lane) = codes_of(y);
-    if ((lane & 15) == 0) *(float*)(row + kDimV + (lane >> 2)) = __builtin_bit_cast(float, (uint32_t)(e + 127) << 23);
-    *(uint16_t*)(row + kDimV + 16 + 2 * lane) = (uint16_t)pack_bf16x2(r, 0.f);
+    for (int i = 0; i < 8; ++i) top = max(top, magnitude(y[i]));
+    if (FORMAT == SPLASH_KV_FP8_E4M3) top = max(top, magnitude(r));
+    if (!__any(top >= kInfinite)) write_row<FORMAT, true>(a, slot, lane, y, r, top);
+    else write_row<FORMAT, false>(a, slot, lane, y, r, top);
   }
 }
 
