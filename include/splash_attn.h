@@ -691,20 +691,20 @@ int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stri
  *   q_indptr, kv_indptr   int32 [batch+1], not decreasing; what lies past num_rows
  *         or num_keys is cut off.  Query rows outside [q_indptr[0], q_indptr[batch])
  *         are left as they are
- *   out   bf16 [num_rows, num_heads, 128] (round to nearest even)
+ *   out   bf16 [num_rows, num_heads, 128] (round to nearest even), over none of the
+ *         inputs
  *   lse   fp32 [num_rows, num_heads]; may be NULL
  *   workspace   splash_mla_prefill_workspace_size bytes, 16-byte aligned; it holds
  *         what one call leaves for its own second launch, and calls that may overlap
  *         take one each
  * Products are summed in fp32; a weight is rounded to bf16 where it meets V (2^-8),
- * its sum is not.  Keys that a row does not see
- * do not touch it, whatever they hold (NaN and infinities in k, key and v among
- * them); a score that is NaN or +inf makes its row NaN.  Deterministic: the same
- * inputs and sizes give the same bits.
+ * its sum is not.  Keys that a row does not see do not touch it, whatever they hold
+ * (NaN and infinities in k, key and v among them); a score that is NaN or +inf makes
+ * its row NaN.  Deterministic: the same inputs and sizes give the same bits.
  * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, softmax_scale not
  * finite and > 0), UNSUPPORTED (num_heads past 1024, num_rows or num_keys past 2^25,
  * batch past 2^20, a token stride past 2^24, num_rows * num_heads past 2^31 - 1,
- * (num_rows / 128 + batch) * num_heads past 2^21),
+ * (num_rows / 128 + min(batch, num_rows)) * num_heads past 2^21),
  * MISALIGNED (tensors or workspace not 16-byte, strides not multiples of 8, other
  * arrays not 4-byte aligned), WORKSPACE_TOO_SMALL.
  */
