@@ -17,6 +17,7 @@ constexpr int kRopePairs = kRope / 2;
 struct TurnLaunch {
   const int32_t* positions;   // nullptr: rows are taken as they are
   int64_t position_stride;
+  int32_t axes;               // 1: axis is all 0
   int32_t interleaved;
   float scale;
   double turns[kRopePairs];   // inv_freq / (2 pi): turns per position

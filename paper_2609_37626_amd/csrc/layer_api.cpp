@@ -58,6 +58,7 @@ int read_turn(const splash_rope_desc* rope, const int32_t* positions, int64_t po
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "position_stride must be 0 or at least num_tokens");
   t->positions = positions;
   t->position_stride = position_stride;
+  t->axes = rope->num_axes;
   t->interleaved = rope->interleaved ? 1 : 0;
   t->scale = rope->scale;
   return SPLASH_OK;

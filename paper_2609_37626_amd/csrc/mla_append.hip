@@ -11,10 +11,11 @@
 // it to their order.
 //
 // Bound: the instructions of a token, then HBM: 11.1k tokens into per-token E4M3 take
-// 8.9 us for 19 MB (2.8 us at the rate of reads).  Sums and maxima over lanes by row
-// turns and lane reads rather than shuffles through LDS, 1 / sqrt by two Newton steps,
-// quotients by one inverse and a correction and finite values on a path of their own took
-// it from 11.0 us.  A token for each of 256 requests is launch latency: 3.5 us.
+// 8.2 us for 19 MB (2.8 us at the rate of reads).  From 11.0 us: sums and maxima over
+// lanes by row turns and lane reads rather than shuffles through LDS, 1 / sqrt by two
+// Newton steps, quotients by one inverse and a correction, finite values on a path of
+// their own (to 9.5), and every load of a token before the first wait (to 8.2).  A token
+// for each of 256 requests is launch latency: 3.4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -89,17 +90,15 @@ __device__ __forceinline__ double inverse_root(double x) {
   s = s * __builtin_fma(-h * s, s, 1.5);
   return r > 0.0 && r < __builtin_inf() ? s : r;  // (x infinite, zero or NaN: r itself)
 }
-// The quotients by one scale, as a division gives them: the product with its inverse and
-// one correction (below 2^-100 the residual would leave fp32's range: a division).
-struct Quotient {
-  float scale, inverse;
-  bool small;
-  __device__ __forceinline__ float operator()(float y) const {
-    if (small) return y / scale;
-    const float q = y * inverse;
-    return fabsf(q) < 1e30f ? copysignf(__builtin_fmaf(__builtin_fmaf(-q, scale, y), inverse, q), y) : q;
-  }
-};
+// y / scale as a division gives it, by scale's inverse: their product and one correction
+// (compared with the division over all of scale's fractions, at and beside the ties of
+// E4M3).  scale >= 2^-100, below which what is left over would pass fp32's range.
+template <bool FINITE>
+__device__ __forceinline__ float quotient(float y, float scale, float inverse) {
+  const float q = y * inverse;
+  const float r = copysignf(__builtin_fmaf(__builtin_fmaf(-q, scale, y), inverse, q), y);
+  return FINITE || fabsf(q) < 1e30f ? r : q;
+}
 
 // A token's row into the pool.  FINITE: no infinity and no NaN among its values.
 template <int FORMAT, bool FINITE>
@@ -113,12 +112,19 @@ __device__ __forceinline__ void write_row(const MlaAppendLaunch& a, int32_t slot
   if constexpr (FORMAT == SPLASH_KV_FP8_E4M3) {
     const float largest = __builtin_bit_cast(float, wave_max(top));
     const float scale = largest > 0.f ? fmaxf(largest / kTop, 0x1p-126f) : 1.f;
-    const Quotient over = {scale, 1.f / scale, scale < 0x1p-100f};
+    if (scale >= 0x1p-100f) {
+      const float inverse = 1.f / scale;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = over(y[i]);
+      for (int i = 0; i < 8; ++i) y[i] = quotient<FINITE>(y[i], scale, inverse);
+      r = quotient<FINITE>(r, scale, inverse);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] /= scale;
+      r /= scale;
+    }
     uint8_t* row = a.pages + (int64_t)slot * kDimQK;
     *(u32x2*)(row + 8 * lane) = codes_of<FINITE>(y);
-    row[kDimV + lane] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(held<FINITE>(over(r)), 0.f, 0, false);
+    row[kDimV + lane] = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(held<FINITE>(r), 0.f, 0, false);
     if (lane == 0) a.scales[slot] = scale;
   } else {
     // a quarter's 128 columns are 16 lanes; the least e with top <= 1.75 * 2^(e + 8), by
@@ -140,10 +146,20 @@ __global__ __launch_bounds__(kThreads) void mla_append_kernel(MlaAppendLaunch a)
   const int lane = threadIdx.x & 63;
   const int64_t n = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (n >= a.num_tokens) return;
-  const int32_t slot = __builtin_amdgcn_readfirstlane(a.slots[n]);
+  // all of the token's loads before the first wait
+  int none = 0;
+  asm volatile("" : "+v"(none));  // (a vector load: a scalar one would be waited for with the arguments)
+  int32_t slot = a.slots[n + none];
   const u32x4 raw = *(const u32x4*)(a.latent + n * a.latent_stride + 8 * lane);
-  const float key = __builtin_bit_cast(float, (uint32_t)a.key[n * a.key_stride + lane] << 16);
+  const uint32_t key_bits = a.key[n * a.key_stride + lane];
+  u32x4 w = {0u, 0u, 0u, 0u};
+  if (a.norm_weight) w = *(const u32x4*)(a.norm_weight + 8 * lane);
+  PairAngle angle = {0, 0.0};
+  if (a.turn.positions) angle = pair_angle(a.turn, n, pair_of(a.turn, lane));
+  asm volatile("" ::"v"(slot), "v"(raw), "v"(key_bits), "v"(w), "v"(angle.position), "v"(angle.turns));
+  slot = __builtin_amdgcn_readfirstlane(slot);
   if (slot < 0 || (slot >> 6) >= a.num_pages) return;
+  const float key = __builtin_bit_cast(float, key_bits << 16);
   float x[8], y[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -153,11 +169,10 @@ __global__ __launch_bounds__(kThreads) void mla_append_kernel(MlaAppendLaunch a)
   float r = key;
   if (a.turn.positions) {
     float c, s;
-    pair_turn(a.turn, n, pair_of(a.turn, lane), c, s);
+    pair_turn(a.turn, angle, c, s);
     r = turn_element(a.turn, lane, key, c, s);
   }
   if (a.norm_weight) {
-    const u32x4 w = *(const u32x4*)(a.norm_weight + 8 * lane);
     double squares = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) squares = __builtin_fma((double)x[i], (double)x[i], squares);

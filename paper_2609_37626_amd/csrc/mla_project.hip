@@ -52,7 +52,7 @@ __device__ __forceinline__ void turn_heads(const MlaAbsorbLaunch& a, int64_t n, 
   uint16_t* out = a.out + n * a.heads * kDimQK + kDimV;
   const int32_t end = min(first + kHeads, a.heads);
   const bool turned = a.turn.positions != nullptr;
-  if (turned && lane < kRopePairs) pair_turn(a.turn, n, lane, cosine[lane], sine[lane]);
+  if (turned && lane < kRopePairs) pair_turn(a.turn, pair_angle(a.turn, n, lane), cosine[lane], sine[lane]);
   __builtin_amdgcn_wave_barrier();  // (one wave's LDS is in order)
   if (!turned || a.turn.interleaved) {
     const int piece = lane & 7;

@@ -5,12 +5,22 @@
 
 namespace splash {
 
-// Sine and cosine (times the turn's scale) of pair j at token n.  The angle in
-// turns, position * inv_freq / (2 pi), is formed and reduced to [-1/2, 1/2] in 64
-// bits (in 32, position 2^20 would leave 2^-4 rad of it); what is left goes
-// through fp32, 2^-22 or less of a pair.
-__device__ __forceinline__ void pair_turn(const TurnLaunch& t, int64_t n, int j, float& cosine, float& sine) {
-  double turns = (double)t.positions[t.axis[j] * t.position_stride + n] * t.turns[j];
+// What pair j's angle at token n is made of.
+struct PairAngle {
+  int32_t position;
+  double turns;  // a position
+};
+__device__ __forceinline__ PairAngle pair_angle(const TurnLaunch& t, int64_t n, int j) {
+  const int64_t axis = t.axes > 1 ? t.axis[j] * t.position_stride : 0;
+  return {t.positions[axis + n], t.turns[j]};
+}
+
+// Its sine and cosine, times the turn's scale.  The angle in turns, position *
+// inv_freq / (2 pi), is formed and reduced to [-1/2, 1/2] in 64 bits (in 32, position
+// 2^20 would leave 2^-4 rad of it); what is left goes through fp32, 2^-22 or less of a
+// pair.
+__device__ __forceinline__ void pair_turn(const TurnLaunch& t, PairAngle angle, float& cosine, float& sine) {
+  double turns = (double)angle.position * angle.turns;
   turns -= __builtin_rint(turns);
   float s, c;
   sincospif(2.f * (float)turns, &s, &c);
