@@ -1,22 +1,37 @@
 // gfx950 kernel of splash_mla_prefill: causal attention of ragged prompts over
 // expanded keys (128 of a head's own dims, 64 shared rotary ones) and values.
 //
-// A workgroup takes 128 query rows of a request and head, 32 a wave, and walks over
-// the keys 64 at a time; a step's keys and values come straight into LDS, the next
-// step's while this one is multiplied.
+// A workgroup of W waves takes a tile of 32 W query rows of a request and head, 32 a
+// wave, and walks over the keys in steps of 64 whose keys and values come straight into
+// LDS, the next steps' while this one is multiplied; a step is two turns of 32 keys.
 //   QK  S^T[key, row] = K Q^T, v_mfma_f32_16x16x32_bf16.  Lane (g, c) holds keys
 //       16 t + 4 g + i of row c: the weights of a row stay in its four lanes.
-//   PV  O^T[value, row] = V^T P^T.  The product's slot (g, j) is key 4 g + j of tile
-//       2 u (j < 4) or 4 g + j - 4 of tile 2 u + 1: P goes from QK's result to PV's
-//       operand in the lane that has it, and V's transposing reads take the rows
-//       in that order.
-// The softmax runs over the steps once with a reference that moves only where a
-// score passes it by 2^8: below that the weights' sums cannot overflow, and rows that
-// do not move it need no exchange between lanes.
+//   PV  O^T[value, row] = V^T P^T.  The product's slot (g, j) is key 4 g + j of tile 0
+//       (j < 4) or 4 g + j - 4 of tile 1: P goes from QK's result to PV's operand in the
+//       lane that has it, and V's transposing reads take the rows in that order.
+// A turn multiplies QK of its keys while the exponentials of the last turn's scores are
+// dealt out between the matrix instructions, then PV of the last turn: a step's values
+// are the second half of the step before and the first of its own.
 //
-// LDS: two steps' keys, then two steps' values, in line groups of 128 bytes,
-// [group][key][128], chunks of 16 bytes at chunk ^ swz(key); a step's keys are groups
-// 0 and 1 for the head's own dims and 2 for the rotary ones, its values two more.
+// The softmax runs over the keys once with a reference that moves only where a lane's
+// eight weights of a row pass 1024: below that no sum can overflow, and the lane needs no
+// maximum and no exchange for it, only the sum that it makes anyway (looking for the
+// maximum of every turn cost 5% of the long prompt).  Each row decides by its own
+// scores, so that its result does not depend on its neighbours.
+//
+// Bound: matrix instructions, 320 operations a row and key of a head (192 + 128, twice),
+// at 1.36 PFLOP/s of a large library product.  A prompt of 4 x 4096 rows of 32 heads:
+// 716 us, 960 TFLOP/s.  Of that the matrix instructions alone take 420, the loads into LDS
+// 130, its reads 100 and the softmax 80 that two waves a SIMD do not hide.
+//
+// W = 8: one workgroup fills a compute unit, four steps in LDS, two of them on the way;
+// W = 4: two do, two steps each.  The larger tile halves the loads a row and keeps long
+// walks fed; the smaller one wastes less of the triangle at the end of the keys and of a
+// last tile.
+//
+// LDS: a step's keys, then its values, in line groups of 128 bytes, [group][key][128],
+// chunks of 16 bytes at chunk ^ swz(key); keys are groups 0 and 1 for the head's own dims
+// and 2 for the rotary ones, values two more.
 #include <hip/hip_runtime.h>
 #include <limits.h>
 #include <stdint.h>
@@ -40,12 +55,14 @@ constexpr int kAhead = 4;                     // operands read ahead
 constexpr float kMost = 1024.f;               // a lane's eight weights of a row, before the reference moves
 constexpr float kLowest = -1e30f;             // the reference before any score
 constexpr int32_t kTileCost = 1;              // a tile's fixed work, in steps
-constexpr int32_t kNeverCut = 12;             // steps of the longest tile that is never cut
-constexpr int32_t kLeast = 4;                 // steps a worker of the line
+// A cut tile's parts pass through memory and a second launch joins them (6 us): tiles of
+// at most kNeverCut steps, 768 keys, do not wait as long, and a worker of the line gets
+// kLeast steps or more.
+constexpr int32_t kNeverCut = 12;
+constexpr int32_t kLeast = 4;
+constexpr int64_t kLongest = (int64_t)1 << 50;  // a head's line (2^38 for any indptr that does not decrease)
 constexpr int kSorted = 4;                    // requests a lane that the order of the blocks looks at
 
-// W waves, 32 query rows each: tiles of 32 W rows.  With 8 waves one workgroup fills a
-// compute unit (four steps in LDS, two of them on the way), with 4 two do (two steps in LDS).
 constexpr int kWaveRows = 32;
 constexpr int kBlocks = 2;                    // row blocks of 16 a wave
 constexpr int tile_rows(int W) { return kWaveRows * W; }
@@ -628,7 +645,7 @@ __device__ __forceinline__ int32_t line_workers(const MlaPrefillLaunch& a, const
 }
 // Whether the tiles are cut: where the longest one takes longer than all of them over the chip.
 __device__ __forceinline__ bool is_cut(const MlaPrefillLaunch& a, const Call& call) {
-  return call.longest > kNeverCut && call.longest * (int64_t)a.workers > call.line * a.heads;
+  return call.longest > kNeverCut && call.line <= kLongest && call.longest * (int64_t)a.workers > call.line * a.heads;
 }
 
 // A worker's piece of the line from `place` on.
@@ -794,11 +811,14 @@ hipError_t launch_tiles(const MlaPrefillLaunch& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_mla_prefill(const MlaPrefillLaunch& a, hipStream_t s) {
-  // From the call's averages: whether tiles will be cut, and how long they are.
+  // From the call's averages: W = 8 where tiles will be cut or see 64 steps or more on
+  // average.  Measured (us, W = 4 / 8), cut: 8 heads of 16,384 rows 627 / 572, 20 of 2 x 512
+  // rows over 8192 keys 168 / 144, 32 of 2048 rows 119 / 104; long: 32 heads of 4 x 4096 rows
+  // over 4096 more 1,403 / 1,367; else: 32 of 4 x 4096 rows 716 / 764, of 4 x 1024 90 / 104.
   const int64_t rows = max((int64_t)a.num_rows / a.B, (int64_t)1), keys = max((int64_t)a.num_keys / a.B, rows);
   const int64_t steps = (keys - rows / 2) / kKeys, tiles = (rows + 127) / 128 * a.B * a.heads;
   const bool cut = keys > kNeverCut * kKeys && keys / kKeys * 2 * a.units > tiles * steps;
-  return cut || steps >= 64 ? launch_tiles<8>(a, s) : launch_tiles<4>(a, s);
+  return cut || steps >= 40 ? launch_tiles<8>(a, s) : launch_tiles<4>(a, s);
 }
 
 }  // namespace splash
