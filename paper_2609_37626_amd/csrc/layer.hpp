@@ -82,15 +82,19 @@ struct MlaPrefillLaunch {
   float* lse;
   int32_t units;     // compute units
   int32_t workers;   // (made by the launch) workgroups that the chip holds
-  // workspace: two partial results per worker, and {first row, rows, head, parts} of
+  // workspace: the next place of each XCD's tiles (nullptr: a workgroup takes one tile),
+  // two partial results per worker, and {first row, rows, head, parts} of
   // the tile that it begins and does not end (first row -1: none)
+  int32_t* tickets;  // [8], 128 bytes apart
   int4* joined;      // [workers]
   float* part_ml;    // [2 workers, a tile's rows, 2] reference and sum of a row
   float* part_out;   // [2 workers, a tile's rows, 128]
+  void* tiles;       // the tiles' order where none is cut: kPrefillBlock bytes a block, over the parts
 };
 
 constexpr int32_t kPrefillWorkers = 512;
 constexpr int32_t kPrefillParts = 512 * 128;  // workers times a tile's rows, at most
+constexpr int32_t kPrefillBlock = 32;
 
 hipError_t launch_mla_append(const MlaAppendLaunch& a, hipStream_t s);
 hipError_t launch_mla_gather(const MlaGatherLaunch& a, hipStream_t s);

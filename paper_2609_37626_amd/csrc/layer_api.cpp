@@ -25,6 +25,7 @@ constexpr int32_t kMaxLayerHeads = 1024;
 // tile of 128 rows (and its padding) of a prompt.
 constexpr int64_t kMaxProjectedRows = 1 << 28;
 constexpr int64_t kMaxTiles = 1 << 21;
+static_assert(kMaxTiles * kPrefillBlock <= 2 * (int64_t)kPrefillParts * kValue * 4, "every block's place in the workspace");
 constexpr int64_t kMaxTokenStride = 1 << 24;  // 64 rows' byte offsets fit 32 bits
 
 // The pool's limits beyond validate_mla_desc, and its pages.
@@ -78,12 +79,13 @@ int check_projection(int32_t num_tokens, int32_t num_heads, const void* w, int64
 }
 
 struct PrefillLayout {
-  size_t part_ml, part_out, total;  // the joined tiles' records come first
+  size_t joined, part_ml, part_out, total;  // the tickets come first
 };
 PrefillLayout prefill_layout() {
   const size_t slots = 2 * (size_t)kPrefillParts;
   PrefillLayout l;
-  l.part_ml = sizeof(int4) * kPrefillWorkers;
+  l.joined = 8 * 128;
+  l.part_ml = l.joined + sizeof(int4) * kPrefillWorkers;
   l.part_out = l.part_ml + slots * 2 * sizeof(float);
   l.total = l.part_out + slots * kValue * sizeof(float);
   return l;
@@ -273,9 +275,11 @@ int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const
   a.lse = lse;
   char* ws = static_cast<char*>(workspace);
   const PrefillLayout layout = prefill_layout();
-  a.joined = reinterpret_cast<int4*>(ws);
+  a.tickets = reinterpret_cast<int32_t*>(ws);
+  a.joined = reinterpret_cast<int4*>(ws + layout.joined);
   a.part_ml = reinterpret_cast<float*>(ws + layout.part_ml);
   a.part_out = reinterpret_cast<float*>(ws + layout.part_out);
+  a.tiles = a.part_out;
   a.units = splash_device_workers();
   if (!std::isfinite(a.scale_log2)) return fail(SPLASH_ERR_INVALID_ARGUMENT, "softmax_scale * log2(e) passes fp32");
   const hipError_t e = launch_mla_prefill(a, static_cast<hipStream_t>(stream));

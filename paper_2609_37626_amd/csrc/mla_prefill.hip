@@ -85,6 +85,20 @@ struct Tile {
 struct Request {
   int32_t q0, nq, k0, nk;
 };
+// The kernel's arguments, read again: scalar registers that hold them from one use to the
+// next one far away are missed by the loop between.
+__device__ __forceinline__ MlaPrefillLaunch arguments() {
+  static_assert(sizeof(MlaPrefillLaunch) % 8 == 0, "words");
+  constexpr int kWords = sizeof(MlaPrefillLaunch) / 8;
+  const auto* from = (const __attribute__((address_space(4))) uint64_t*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(from));
+  uint64_t word[kWords];
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) word[i] = from[i];
+  MlaPrefillLaunch a;
+  __builtin_memcpy(&a, word, sizeof(a));
+  return a;
+}
 __device__ __forceinline__ Request request(const MlaPrefillLaunch& a, int32_t b) {
   Request r;
   r.q0 = min(max(a.q_indptr[b], 0), a.num_rows);
@@ -297,33 +311,28 @@ __device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int32_t h,
   return false;
 }
 
-// Softmax and products of a tile's steps [step0, step1) in this workgroup's waves.
+// Softmax and products of a tile's steps [step0, step1) in this workgroup's waves;
+// `before` runs once the first loads are on their way (p still holds the last tile),
+// `after` once the wave has multiplied all that it sees, while others still do.
 struct Piece {
   f32x4 o[8][kBlocks];  // O^T: values 16 d + 4 g + i of rows 16 r + c, over exp2 of the reference
   float top[kBlocks], sum[kBlocks];
 };
 typedef f32x4 Scores[2][kBlocks];  // S^T of a turn's keys: keys 16 t + 4 g + i of rows 16 r + c
 
-template <int W>
-__device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& tile, int32_t step0, int32_t step1, uint8_t* lds, Piece& p) {
+template <int W, typename Before, typename After>
+__device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& tile, int32_t step0, int32_t step1, uint8_t* lds, Piece& p,
+                                       Before before, After after) {
   constexpr int R = kBlocks, kHeld = steps_held(W);
   constexpr bool kEarly = W == 8;  // the next step arrives in the middle of a step's last turn
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));  // (its offsets are made for each tile, not held from one to the next)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
   const int32_t row0 = kWaveRows * wave;            // the wave's first row in the tile
   const int32_t sees0 = tile.first_sees + row0;     // keys that it sees
   // turns up to which the wave sees a key
   const int32_t mine = row0 >= tile.rows ? 2 * step0 : max(2 * step0, min(2 * step1, (sees0 + kWaveRows - 1 + kHalf - 1) / kHalf));
-
-  // Q as B operands: row c of a block of 16, eight dims from 8 g.
-  bf16x8 qf[R][6];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int64_t row = tile.q0 + min(row0 + 16 * r + c, tile.rows - 1);
-    const uint16_t* from = a.q + row * a.q_token + tile.h * a.q_head + 8 * g;
-#pragma unroll
-    for (int s = 0; s < 6; ++s) qf[r][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(from + 32 * s));
-  }
 
   // A step's loads: its keys, and the values of the last step's second half and its own
   // first, as they are multiplied.  A wave brings 64 / W rows, eight a load, of each line
@@ -394,6 +403,20 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
   const uint32_t v_row = 4 * g + (c >> 2);
   const uint32_t v_lane = kKeyBytes + 128 * v_row + 16 * (((c >> 1) & 1) ^ swz(v_row)) + 8 * (c & 1);
 
+  // Q as B operands: row c of a block of 16, eight dims from 8 g.
+  bf16x8 qf[R][6];
+  if (step0 < step1) {
+    load_step(step0);
+    if constexpr (kEarly) load_step(step0 + 1);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = tile.q0 + min(row0 + 16 * r + c, tile.rows - 1);
+      const uint16_t* from = a.q + row * a.q_token + tile.h * a.q_head + 8 * g;
+#pragma unroll
+      for (int s = 0; s < 6; ++s) qf[r][s] = __builtin_bit_cast(bf16x8, *(const u32x4*)(from + 32 * s));
+    }
+  }
+  before();
   f32x4 o[8][R];
   float top[R], sum[R];
 #pragma unroll
@@ -406,11 +429,14 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
 
   typedef const LDS_AS uint8_t* Place;
   const auto place_of = [&](int32_t step) { return (Place)lds + ((step - step0) & (kHeld - 1)) * kStepBytes; };
+  // (the turned chunks' bits are below those that a step's place changes: one lane offset
+  // to hold, not four)
+  const auto apart = [](Place p, uint32_t bits) { return (Place)(uintptr_t)((uint32_t)(uintptr_t)p ^ bits); };
   const auto key_operand = [&](Place buf, int at, int i) {
-    return *(const LDS_AS bf16x8*)(buf + (k_lane ^ (64 * (i >> 1 & 1))) + kGroupBytes * (i >> 2) + 2048 * (i & 1) + at);
+    return *(const LDS_AS bf16x8*)(apart(buf + k_lane, 64 * (i >> 1 & 1)) + kGroupBytes * (i >> 2) + 2048 * (i & 1) + at);
   };
   const auto value_operand = [&](Place buf, int at, int d) {
-    Place from = buf + (v_lane ^ (32 * (d & 3))) + kGroupBytes * (d >> 2) + at;
+    Place from = apart(buf + v_lane, 32 * (d & 3)) + kGroupBytes * (d >> 2) + at;
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)from);
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s16x4 LDS_AS*)(from + 2048));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -547,13 +573,16 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < R; ++r) z1[t][r] = (f32x4){-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    load_step(step0);
     if constexpr (kEarly) {
-      load_step(step0 + 1);
       arrive(step0);
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) kf[i] = key_operand(place_of(step0), 0, i);
     }
+    // (the compiler waits for the queries here, not at every turn)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int i = 0; i < 6; ++i) asm volatile("" ::"v"(qf[r][i]));
     // (the wave's last step)
     const int32_t last = mine > 2 * step0 ? mine / 2 : step0 - 1;
     int32_t step = step0;
@@ -569,8 +598,11 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
         turn(2 * step + 1, z1, z0, no, yes);
       }
     }
+    after();
     for (step = last + (kEarly ? 2 : 1); step <= step1; ++step) arrive(step);  // (the other waves' steps)
     wait_vmcnt<0>();  // (nothing of this piece's lands in the next one's)
+  } else {
+    after();
   }
   if (__any(odd)) {
     // (the first turn's values, and from the last turn without masks on)
@@ -613,11 +645,20 @@ __device__ __forceinline__ void write_rows(const MlaPrefillLaunch& a, const Tile
     if (row >= tile.rows) continue;
     const float by = 1.f / l;
     const int64_t n = (tile.q0 + row) * a.heads + tile.h;
-    uint16_t* to = a.out + n * kValue + 4 * g;
+    // Lanes g = 0, 1 and 2, 3 exchange halves of two neighbouring blocks of 16 values:
+    // eight in a row for each, 64 bytes of a row a store.
+    uint16_t* to = a.out + n * kValue + 16 * (g & 1) + 8 * (g >> 1);
 #pragma unroll
-    for (int d = 0; d < 8; ++d) {
-      const f32x4 v = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : p.o[d][r] * by;
-      *(u32x2*)(to + 16 * d) = (u32x2){pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    for (int d = 0; d < 8; d += 2) {
+      u32x2 v[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f32x4 x = l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : p.o[d + k][r] * by;
+        v[k] = (u32x2){pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+      }
+      const auto lo = __builtin_amdgcn_permlane16_swap(v[0][0], v[1][0], false, false);
+      const auto hi = __builtin_amdgcn_permlane16_swap(v[0][1], v[1][1], false, false);
+      *(u32x4*)(to + 16 * d) = (u32x4){lo[0], hi[0], lo[1], hi[1]};
     }
     if (a.lse && g == 0) a.lse[n] = l == 0.f ? -INFINITY : (p.top[r] + __log2f(l)) * 0.69314718055994530942f;
   }
@@ -684,75 +725,177 @@ __device__ __forceinline__ Span find_span(const MlaPrefillLaunch& a, const Call&
   return s;
 }
 
-// Whole tiles, a workgroup each, or the line of all tiles in equal spans.
+// What the tiles' order is looked up in: the block of every rank; `blocks` of them.
+// a.tiles lies where a cut call's parts do.
+struct Block {
+  Request r;
+  int32_t block;  // of its request, from the last one on
+  int32_t none[3];
+};
+static_assert(sizeof(Block) == kPrefillBlock, "the workspace's");
+// One wave a rank; past the requests that are ordered, one workgroup for all requests.
+template <int ROWS>
+__global__ __launch_bounds__(kThreads) void mla_prefill_order_kernel(MlaPrefillLaunch a, int32_t shift, int32_t blocks) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Block* to = (Block*)a.tiles;
+  if (blockIdx.x == 0 && threadIdx.x < 8) a.tickets[32 * threadIdx.x] = 0;
+  if (a.B <= 64 * kSorted) {
+    const int32_t rank = (int32_t)blockIdx.x * (kThreads / 64) + wave;
+    if (rank >= blocks) return;
+    Block b = {};
+    if (!find_block<ROWS>(a, rank, shift, b.r, b.block)) b.r.nq = 0;
+    if (lane == 0) to[rank] = b;
+    return;
+  }
+  __shared__ int32_t sums[kThreads / 64];
+  int64_t behind = 0;
+  for (int32_t b0 = 0; b0 < a.B && behind < blocks; b0 += kThreads) {
+    const int32_t at = b0 + (int32_t)threadIdx.x;
+    const Request r = request(a, min(at, a.B - 1));
+    const int32_t own = at < a.B ? (tiles_of<ROWS>(r.nq) + (1 << shift) - 1) >> shift : 0, upto = wave_prefix(own);
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int64_t first = behind + upto - own;
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; ++k) {
+      if (k < wave) first += sums[k];
+      behind += sums[k];
+    }
+    __syncthreads();
+    for (int32_t k = 0; k < own && first + k < blocks; ++k) to[first + k] = Block{r, k, {}};
+  }
+  for (int64_t k = behind + threadIdx.x; k < blocks; k += kThreads) to[k] = Block{};
+}
+
+// Whole tiles, or the line of all tiles in equal spans.  A workgroup takes one tile, or
+// (where there are more than the chip holds, with a.tickets) one after the other: a new
+// workgroup would begin 10 us after the last one's end on its compute unit, with nothing
+// on the way.  The first wave, whose rows see the fewest keys, finds the next tile while
+// the others still multiply; its first step and queries are loaded before the last
+// tile's rows are written.
 template <int W>
-__global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch a, int32_t shift) {
+__global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch a, int32_t shift, int32_t blocks) {
   __shared__ __align__(128) uint8_t lds[steps_held(W) * kStepBytes];
   constexpr int ROWS = tile_rows(W);
-  int32_t w = -1;             // the worker on the line (-1: a whole tile)
-  int64_t place = -1;
-  Tile tile;
-  int32_t step0 = 0, step1;
-  {
-    const int32_t xcd = blockIdx.x & 7, at = blockIdx.x >> 3;   // (workgroups go round the 8 XCDs)
-    if (a.joined) {
-      const Call call = look_at<ROWS>(a);
-      if (is_cut(a, call)) {
-        const int32_t each = line_workers(a, call) / 8;
-        if (at < each) w = xcd * each + at;  // neighbours on the line on one XCD
-      }
-      if (w < 0) {
-        if (blockIdx.x < (uint32_t)a.workers && threadIdx.x == 0) a.joined[blockIdx.x] = make_int4(-1, 0, 0, 0);
-        if (is_cut(a, call)) return;
-      }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int32_t xcd = blockIdx.x & 7;  // (workgroups go round the 8 XCDs)
+  int32_t w = -1;                      // the worker on the line (-1: whole tiles)
+  Tile tile = {0, 0, 0, 0, 0, 0}, last = tile;
+  if (a.joined) {
+    const Call call = look_at<ROWS>(a);
+    if (is_cut(a, call)) {
+      const int32_t each = line_workers(a, call) / 8, at = blockIdx.x >> 3;
+      if (at < each) w = xcd * each + at;  // neighbours on the line on one XCD
     }
-    if (w < 0) {
-      // Groups of 2^shift tiles of a head, neighbours of one XCD that begin together and
-      // read the same keys; the longest groups first, of all heads.
-      const int64_t group = (int64_t)(at >> shift) * 8 + xcd;
-      Request r;
-      int32_t block;
-      if (!find_block<ROWS>(a, (int32_t)(group / a.heads), shift, r, block)) return;
-      const int32_t i = tiles_of<ROWS>(r.nq) - 1 - (block << shift) - (at & ((1 << shift) - 1));
-      if (i < 0) return;
-      tile = tile_of<ROWS>(r, (int32_t)(group % a.heads), i);
-      step1 = (tile.keys + kKeys - 1) / kKeys;
-    }
+    const uint32_t own = w < 0 ? blockIdx.x : w;
+    if (own < (uint32_t)a.workers && threadIdx.x == 0) a.joined[own] = make_int4(-1, 0, 0, 0);
+    if (w < 0 && is_cut(a, call)) return;
   }
-  int4 record = {-1, 0, 0, 0};
+  // Groups of 2^shift tiles of a head, neighbours of one XCD that begin together and
+  // read the same keys; the longest groups first, of all heads.  False: there is no tile
+  // at this place of the XCD's; rank: its block's.
+  const auto tile_at = [&](int32_t at, const Request& r, int32_t block, Tile& t) {
+    const int32_t i = tiles_of<ROWS>(r.nq) - 1 - (block << shift) - (at & ((1 << shift) - 1));
+    if (i < 0) return false;
+    t = tile_of<ROWS>(r, (int32_t)(((int64_t)(at >> shift) * 8 + xcd) % a.heads), i);
+    return true;
+  };
+  const auto rank_of = [&](int32_t at) { return ((int64_t)(at >> shift) * 8 + xcd) / a.heads; };
+  if (w < 0 && !a.tickets) {
+    Request r;
+    int32_t block;
+    const int32_t at = blockIdx.x >> 3;
+    if (!find_block<ROWS>(a, (int32_t)rank_of(at), shift, r, block) || !tile_at(at, r, block, tile)) return;
+  }
+  // The next tile, in lanes: rows (0: there are no more), q0, k0, first_sees, keys, h.
+  volatile int32_t kept;  // (in memory: the loops have no register for it)
+  bool first = true;
+  const auto find = [&] {
+    int32_t told[6] = {};
+    while (true) {
+      const MlaPrefillLaunch a = arguments();
+      int32_t at = blockIdx.x >> 3;
+      if (!first) {
+        int32_t ticket = 0;
+        if (lane == 0) ticket = __hip_atomic_fetch_add(a.tickets + 32 * xcd, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        at = (int32_t)(gridDim.x >> 3) + __builtin_amdgcn_readfirstlane(ticket);
+      }
+      first = false;
+      const int64_t rank = rank_of(at);
+      if (rank >= blocks) break;
+      const Block b = ((const Block*)a.tiles)[rank];
+      if (b.r.nq == 0) break;
+      Tile t;
+      if (!tile_at(at, b.r, b.block, t)) continue;
+      told[0] = t.rows;
+      told[1] = (int32_t)t.q0;
+      told[2] = (int32_t)t.k0;
+      told[3] = t.first_sees;
+      told[4] = t.keys;
+      told[5] = t.h;
+      break;
+    }
+    int32_t found = 0;
+#pragma unroll
+    for (int k = 0; k < 6; ++k) found = lane == k ? told[k] : found;
+    kept = found;
+  };
+  int64_t place = -1;
+  int32_t step0 = 0, step1 = (tile.keys + kKeys - 1) / kKeys;
   Piece p;
   while (true) {
     if (w >= 0) {
-      const Span s = find_span<ROWS>(a, look_at<ROWS>(a), w, place);
+      const MlaPrefillLaunch b = arguments();
+      const Span s = find_span<ROWS>(b, look_at<ROWS>(b), w, place);
       if (place >= 0) lds_barrier();  // nobody reads the last piece's keys any more
       tile = s.tile;
       step0 = s.step0;
       step1 = s.step1;
     }
-    attend<W>(a, tile, step0, step1, lds, p);
+    attend<W>(
+        arguments(), tile, step0, step1, lds, p,
+        [&] {
+          if (last.rows > 0) write_rows(arguments(), last, p);
+        },
+        [&] {
+          if (w < 0 && wave == 0 && a.tickets) find();
+        });
     if (w < 0) {
-      write_rows(a, tile, p);
+      const MlaPrefillLaunch b = arguments();
+      last = tile;
+      if (b.tickets) {
+        int32_t* told = (int32_t*)(lds + (steps_held(W) - 1) * kStepBytes);  // (the next first steps go elsewhere)
+        lds_barrier();  // nobody reads keys any more
+        if (wave == 0 && lane < 6) told[lane] = kept;
+        lds_barrier();
+        const int4 t0 = *(const int4*)told;
+        const int2 t1 = *(const int2*)(told + 4);
+        tile = Tile{uniform(t1.y, 0), uniform(t0.x, 0), uniform(t0.y, 0), uniform(t0.z, 0), uniform(t0.w, 0), uniform(t1.x, 0)};
+        step1 = (tile.keys + kKeys - 1) / kKeys;
+        if (tile.rows > 0) continue;
+      }
+      if (last.rows > 0) write_rows(b, last, p);
       return;
     }
     // (found again: held beside the loop above, it would cost its registers)
     asm volatile("" : "+s"(place));
-    const Span s = find_span<ROWS>(a, look_at<ROWS>(a), w, place);
+    const MlaPrefillLaunch b = arguments();
+    const Span s = find_span<ROWS>(b, look_at<ROWS>(b), w, place);
     if (s.begins && s.ends) {
-      write_rows(a, s.tile, p);
+      write_rows(b, s.tile, p);
     } else {
-      write_part<W>(a, s.tile, p, 2 * w + (s.begins ? 1 : 0));
+      write_part<W>(b, s.tile, p, 2 * w + (s.begins ? 1 : 0));
       if (s.begins) {
         // the parts of this tile: this one, and one of each worker up to its end
-        int32_t last = w + 1;
-        while (span_at(s.length, s.workers, last + 1) < s.tile_end) ++last;
-        record = make_int4((int32_t)s.tile.q0, s.tile.rows, s.tile.h, last - w + 1);
+        int32_t upto = w + 1;
+        while (span_at(s.length, s.workers, upto + 1) < s.tile_end) ++upto;
+        if (threadIdx.x == 0) b.joined[w] = make_int4((int32_t)s.tile.q0, s.tile.rows, s.tile.h, upto - w + 1);
       }
     }
     wait_vmcnt<0>();  // (the parts' stores, before loads are counted again)
     place = s.tile_end;
-    if (place >= s.end) break;
+    if (place >= s.end) return;
   }
-  if (threadIdx.x == 0) a.joined[w] = record;
 }
 
 // The parts of the tile that worker blockIdx.x begins, 16 rows a workgroup: sixteen
@@ -803,7 +946,15 @@ hipError_t launch_tiles(const MlaPrefillLaunch& a, hipStream_t s) {
   int64_t groups = (blocks * a.heads + 7) / 8 * 8 << shift;
   if (a.num_keys <= kNeverCut * kKeys) l.joined = nullptr;
   else groups = max(groups, (int64_t)l.workers);
-  hipLaunchKernelGGL((mla_prefill_kernel<W>), dim3((unsigned)groups), dim3(64 * W), 0, s, l, shift);
+  if (groups > l.workers) {
+    groups = l.workers;
+    const int64_t waves = a.B <= 64 * kSorted ? blocks : 1;
+    hipLaunchKernelGGL((mla_prefill_order_kernel<kRows>), dim3((unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64))), dim3(kThreads), 0, s,
+                       l, shift, (int32_t)blocks);
+  } else {
+    l.tickets = nullptr;
+  }
+  hipLaunchKernelGGL((mla_prefill_kernel<W>), dim3((unsigned)groups), dim3(64 * W), 0, s, l, shift, (int32_t)blocks);
   if (l.joined) hipLaunchKernelGGL((mla_prefill_join_kernel<kRows>), dim3((unsigned)l.workers, kRows / 16), dim3(kThreads), 0, s, l);
   return hipGetLastError();
 }
