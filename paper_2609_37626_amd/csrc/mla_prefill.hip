@@ -15,14 +15,16 @@
 //
 // The softmax runs over the keys once with a reference that moves only where a lane's
 // eight weights of a row pass 1024: below that no sum can overflow, and the lane needs no
-// maximum and no exchange for it, only the sum that it makes anyway (looking for the
-// maximum of every turn cost 5% of the long prompt).  Each row decides by its own
-// scores, so that its result does not depend on its neighbours.
+// maximum and no exchange for it, only the sum that it makes anyway.  Each row decides by
+// its own scores, so that its result does not depend on its neighbours.
 //
-// Bound: matrix instructions, 320 operations a row and key of a head (192 + 128, twice),
-// at 1.36 PFLOP/s of a large library product.  A prompt of 4 x 4096 rows of 32 heads:
-// 716 us, 960 TFLOP/s.  Of that the matrix instructions alone take 420, the loads into LDS
-// 130, its reads 100 and the softmax 80 that two waves a SIMD do not hide.
+// Bound: matrix instructions, 320 multiplications and additions each a row and key of a
+// head (192 + 128), at 1.36 PFLOP/s of a large library product.  128 heads of one prompt
+// of 4096 rows: 703 us, 978 TFLOP/s; 32 of 2 x 4096 rows over 4096 more: 889 us, 1,160.
+// Of the first, the matrix instructions alone take 420 us, the loads into LDS 130, its
+// reads 100 and the softmax 80 that two waves a SIMD do not hide; a tile costs 8 us beside
+// its turns (loads of its first step and queries 3.4, writing the last one's rows 3.6, the
+// meeting of its waves 1.1), and its masked turns half as much again as others.
 //
 // W = 8: one workgroup fills a compute unit, four steps in LDS, two of them on the way;
 // W = 4: two do, two steps each.  The larger tile halves the loads a row and keeps long
@@ -197,7 +199,7 @@ __device__ __forceinline__ Call look_at(const MlaPrefillLaunch& a) {
   return {wave_sum(line), wave_max(longest)};
 }
 
-// Block `rank` of the requests' blocks of 2^shift tiles, counted from a request's last
+// Block number `rank` of the requests' blocks of 2^shift tiles, counted from a request's last
 // tile, the longest first: which of its request's and of which request (false: none).
 // Block j counts as K - D j steps, K its request's last tile's: how many
 // blocks are longer than a length is a sum over the requests, and the rank's length
@@ -962,10 +964,11 @@ hipError_t launch_tiles(const MlaPrefillLaunch& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_mla_prefill(const MlaPrefillLaunch& a, hipStream_t s) {
-  // From the call's averages: W = 8 where tiles will be cut or see 64 steps or more on
-  // average.  Measured (us, W = 4 / 8), cut: 8 heads of 16,384 rows 627 / 572, 20 of 2 x 512
-  // rows over 8192 keys 168 / 144, 32 of 2048 rows 119 / 104; long: 32 heads of 4 x 4096 rows
-  // over 4096 more 1,403 / 1,367; else: 32 of 4 x 4096 rows 716 / 764, of 4 x 1024 90 / 104.
+  // From the call's averages: W = 8 where tiles will be cut or see 40 steps or more on
+  // average.  Measured (us, W = 4 / 8), cut: 8 heads of 16,384 rows 606 / 567, 20 of 2 x 512
+  // rows over 8192 keys 168 / 137, of 8 x 200 over 4000 174 / 143; long: 128 of 6144 rows
+  // 1,522 / 1,490, 32 of 8 x 1024 over 4096 784 / 721; else: 128 of 4096 rows 714 / 721, 32
+  // of 4 x 1024 83 / 96, 16 of 64 x 200 91 / 106.
   const int64_t rows = max((int64_t)a.num_rows / a.B, (int64_t)1), keys = max((int64_t)a.num_keys / a.B, rows);
   const int64_t steps = (keys - rows / 2) / kKeys, tiles = (rows + 127) / 128 * a.B * a.heads;
   const bool cut = keys > kNeverCut * kKeys && keys / kKeys * 2 * a.units > tiles * steps;
