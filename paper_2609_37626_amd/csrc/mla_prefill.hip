@@ -24,7 +24,7 @@
 // Of the first, the matrix instructions alone take 420 us, the loads into LDS 130, its
 // reads 100 and the softmax 80 that two waves a SIMD do not hide; a tile costs 8 us beside
 // its turns (loads of its first step and queries 3.4, writing the last one's rows 3.6, the
-// meeting of its waves 1.1), and its masked turns half as much again as others.
+// meeting of its waves 1.1), and a masked turn has 440 vector instructions, others 260.
 //
 // W = 8: one workgroup fills a compute unit, four steps in LDS, two of them on the way;
 // W = 4: two do, two steps each.  The larger tile halves the loads a row and keeps long
@@ -909,21 +909,35 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
   const int32_t row = blockIdx.y * 16 + (threadIdx.x >> 4), lane = threadIdx.x & 15;
   if (record.x < 0 || row >= record.y) return;
   const auto slot = [&](int32_t k) { return ((int64_t)(k == 0 ? 2 * w + 1 : 2 * (w + k)) * ROWS + row); };
-  float top = kLowest;
-  for (int32_t k = 0; k < record.w; ++k) {
-    const float m = a.part_ml[slot(k) * 2];
-    top = m > top || m != m ? m : top;
-  }
+  // (four parts' loads at once; a part without a weight holds zeros)
+  float top = kLowest, sum = 0.f;
   f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-  float sum = 0.f;
-  for (int32_t k = 0; k < record.w; ++k) {
-    const f32x2 ml = *(const f32x2*)(a.part_ml + slot(k) * 2);
-    if (ml[1] == 0.f) continue;  // no weight, and nothing in its output
-    const float by = __builtin_amdgcn_exp2f(ml[0] - top);
-    const f32x4* from = (const f32x4*)(a.part_out + slot(k) * kValue + 8 * lane);
-    sum += by * ml[1];
-    lo += by * from[0];
-    hi += by * from[1];
+  for (int32_t k0 = 0; k0 < record.w; k0 += 4) {
+    f32x2 ml[4];
+    f32x4 v[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at = slot(min(k0 + i, record.w - 1));
+      ml[i] = *(const f32x2*)(a.part_ml + at * 2);
+      v[i][0] = *(const f32x4*)(a.part_out + at * kValue + 8 * lane);
+      v[i][1] = *(const f32x4*)(a.part_out + at * kValue + 8 * lane + 4);
+    }
+    float to = top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) to = ml[i][0] > to || ml[i][0] != ml[i][0] ? ml[i][0] : to;
+    const float old = __builtin_amdgcn_exp2f(top - to);
+    top = to;
+    sum *= old;
+    lo *= old;
+    hi *= old;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (k0 + i >= record.w) break;
+      const float by = __builtin_amdgcn_exp2f(ml[i][0] - to);
+      sum += by * ml[i][1];
+      lo += by * v[i][0];
+      hi += by * v[i][1];
+    }
   }
   const int64_t n = (int64_t)(record.x + row) * a.heads + record.z;
   const float by = sum == 0.f ? 0.f : 1.f / sum;
