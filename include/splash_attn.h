@@ -25,7 +25,9 @@
  * (splash_mla_combine), and around the same core: one position shard of the
  * histories (splash_mla_attend_shard), attention over listed positions only
  * (splash_mla_attend_topk), and the DOP regroup of query and output rows
- * (splash_dop_*).
+ * (splash_dop_*).  Beside it, each in a section of its own below: the serving step
+ * around grouped-query attention, and the latent-attention layer around this cache
+ * (the rows' way in and out, the projections, a prompt's expanded attention).
  *
  * Conventions for every entry point:
  *  - All tensor pointers are DEVICE pointers owned by the caller; the library
