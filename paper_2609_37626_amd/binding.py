@@ -655,8 +655,9 @@ def splash_mla_append(latent, key, slots, kv_pages, kv_scales, desc: MlaDesc, no
         _refuse_pool(desc, dev, kv_pages, slots=(slots, (_I32T,), (n,)), norm_weight=(norm_weight, (_BF16T,), (512,)),
                      kv_scales=(kv_scales if fp8 else None, (_F32T,), (pages, 64)))
     at, stride = _NO_TURN if rope is None else _turn_args(positions, rope, n, dev)
+    # (of one row the stride may be anything)
     _on_device(dev, lib().splash_mla_append, (
-        latent.data_ptr(), ls[0], key.data_ptr(), ks[0], None if norm_weight is None else norm_weight.data_ptr(), norm_eps,
+        latent.data_ptr(), ls[0] if n > 1 else 512, key.data_ptr(), ks[0] if n > 1 else 64, None if norm_weight is None else norm_weight.data_ptr(), norm_eps,
         at, stride, rope, slots.data_ptr(), n, kv_pages.data_ptr(), kv_scales.data_ptr() if fp8 else None, desc), stream)
 
 
