@@ -278,9 +278,9 @@ __device__ __forceinline__ bool find_block(const MlaPrefillLaunch& a, int32_t ra
   return false;
 }
 
-// The tile that holds place `at` of a head's line, and where it begins.
+// The tile that holds place `at` of a head's line: its request, which of it, and where it begins.
 template <int ROWS>
-__device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int32_t h, int64_t at, Tile& t, int64_t& begin, int32_t& count) {
+__device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int64_t at, Request& r, int32_t& tile, int64_t& begin) {
   const int lane = threadIdx.x & 63;
   int64_t behind = 0;
   for (int32_t b0 = 0; b0 < a.B; b0 += 64) {
@@ -293,7 +293,7 @@ __device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int32_t h,
       continue;
     }
     const int who = __builtin_ctzll(past);
-    const Request r = uniform(mine, who);
+    r = uniform(mine, who);
     behind += uniform(upto - own, who);
     // the last i with line_upto(i) <= at - behind
     const int32_t first = line_first<ROWS>(r);
@@ -304,10 +304,8 @@ __device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int32_t h,
     i = min(max(i, (int64_t)0), (int64_t)tiles_of<ROWS>(r.nq) - 1);
     while (i > 0 && line_upto<ROWS>(i, first) > x) --i;
     while (i + 1 < tiles_of<ROWS>(r.nq) && line_upto<ROWS>(i + 1, first) <= x) ++i;
-    const int32_t ti = __builtin_amdgcn_readfirstlane((int32_t)i);
-    t = tile_of<ROWS>(r, h, ti);
-    begin = behind + line_upto<ROWS>(ti, first);
-    count = first + ROWS / kKeys * ti;
+    tile = __builtin_amdgcn_readfirstlane((int32_t)i);
+    begin = behind + line_upto<ROWS>(tile, first);
     return true;
   }
   return false;
@@ -691,39 +689,83 @@ __device__ __forceinline__ bool is_cut(const MlaPrefillLaunch& a, const Call& ca
   return call.longest > kNeverCut && call.line <= kLongest && call.longest * (int64_t)a.workers > call.line * a.heads;
 }
 
-// A worker's piece of the line from `place` on.
-struct Span {
-  Tile tile;
-  int32_t step0, step1;
-  bool begins, ends;  // the piece begins or ends its tile
-  int64_t first, tile_end, end;  // the worker's first place, the tile's end, the worker's
-  int32_t workers;
-  int64_t length;
-};
+// Worker w's piece of the line: of tile `i` of a request.
 __device__ __forceinline__ int64_t span_at(int64_t length, int32_t workers, int64_t k) {
   return length / workers * k + length % workers * k / workers;
 }
+struct Span {
+  Request r;
+  int32_t i, h;
+  int64_t begin, tile_end, end;  // the tile's place on the line, its end, the worker's end
+  int64_t line;                  // a head's steps
+  int32_t step0, step1;
+  bool begins, ends;  // the piece begins or ends its tile
+};
+// From place on; tile and its begin are known.
 template <int ROWS>
-__device__ __forceinline__ Span find_span(const MlaPrefillLaunch& a, const Call& call, int32_t w, int64_t place) {
-  Span s;
-  s.workers = line_workers(a, call);
-  s.length = call.line * a.heads;
-  s.first = span_at(s.length, s.workers, w);
-  s.end = span_at(s.length, s.workers, w + 1);
-  if (place < 0) place = s.first;
-  const int32_t h = (int32_t)(place / call.line);
-  int64_t begin = 0;
-  int32_t count = 0;
-  s.tile = Tile{h, 0, 0, 0, 0, 0};
-  find_place<ROWS>(a, h, place - h * call.line, s.tile, begin, count);
-  begin += h * call.line;
-  s.tile_end = begin + count;
+__device__ __forceinline__ void cut_piece(Span& s, int64_t place) {
+  const Tile t = tile_of<ROWS>(s.r, s.h, s.i);
+  s.tile_end = s.begin + line_first<ROWS>(s.r) + ROWS / kKeys * s.i;
   // the tile's fixed work comes first on the line, and steps that it lacks last
-  const int32_t steps = (s.tile.keys + kKeys - 1) / kKeys;
-  s.begins = place == begin;
+  const int32_t steps = (t.keys + kKeys - 1) / kKeys;
+  s.begins = place == s.begin;
   s.ends = s.tile_end <= s.end;
-  s.step0 = min(max((int32_t)(place - begin) - kTileCost, 0), steps);
-  s.step1 = s.ends ? steps : min(max((int32_t)(s.end - begin) - kTileCost, 0), steps);
+  s.step0 = min(max((int32_t)(place - s.begin) - kTileCost, 0), steps);
+  s.step1 = s.ends ? steps : min(max((int32_t)(s.end - s.begin) - kTileCost, 0), steps);
+}
+template <int ROWS>
+__device__ __forceinline__ void find_piece(const MlaPrefillLaunch& a, Span& s, int64_t place) {
+  s.h = (int32_t)(place / s.line);
+  s.r = Request{0, 0, 0, 0};
+  s.i = 0;
+  s.begin = 0;
+  find_place<ROWS>(a, place - s.h * s.line, s.r, s.i, s.begin);
+  s.begin += s.h * s.line;
+  cut_piece<ROWS>(s, place);
+}
+// The worker's first piece, and the one after s: the request's next tile, as long as it has one.
+template <int ROWS>
+__device__ __forceinline__ Span first_piece(const MlaPrefillLaunch& a, int32_t w) {
+  const Call call = look_at<ROWS>(a);
+  const int32_t workers = line_workers(a, call);
+  const int64_t length = call.line * a.heads;
+  Span s;
+  s.line = call.line;
+  s.end = span_at(length, workers, w + 1);
+  find_piece<ROWS>(a, s, span_at(length, workers, w));
+  return s;
+}
+template <int ROWS>
+__device__ __forceinline__ void next_piece(const MlaPrefillLaunch& a, Span& s) {
+  if (s.i + 1 < tiles_of<ROWS>(s.r.nq)) {
+    ++s.i;
+    s.begin = s.tile_end;
+    cut_piece<ROWS>(s, s.begin);
+  } else {
+    find_piece<ROWS>(a, s, s.tile_end);
+  }
+}
+// What is needed of it behind the loops, in the lanes of one register.
+__device__ __forceinline__ int32_t in_lanes(const Span& s, int lane) {
+  const int32_t told[13] = {s.r.q0, s.r.nq, s.r.k0, s.r.nk, s.i, s.h, (s.begins ? 1 : 0) | (s.ends ? 2 : 0),
+                            (int32_t)s.tile_end, (int32_t)(s.tile_end >> 32), (int32_t)s.end, (int32_t)(s.end >> 32),
+                            (int32_t)s.line, (int32_t)(s.line >> 32)};
+  int32_t v = 0;
+#pragma unroll
+  for (int k = 0; k < 13; ++k) v = lane == k ? told[k] : v;
+  return v;
+}
+__device__ __forceinline__ Span of_lanes(int32_t v) {
+  const auto wide = [&](int k) { return (int64_t)((uint64_t)(uint32_t)uniform(v, k + 1) << 32 | (uint32_t)uniform(v, k)); };
+  Span s = {};
+  s.r = Request{uniform(v, 0), uniform(v, 1), uniform(v, 2), uniform(v, 3)};
+  s.i = uniform(v, 4);
+  s.h = uniform(v, 5);
+  s.begins = uniform(v, 6) & 1;
+  s.ends = uniform(v, 6) & 2;
+  s.tile_end = wide(7);
+  s.end = wide(9);
+  s.line = wide(11);
   return s;
 }
 
@@ -809,7 +851,8 @@ __global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch
     const int32_t at = blockIdx.x >> 3;
     if (!find_block<ROWS>(a, (int32_t)rank_of(at), shift, r, block) || !tile_at(at, r, block, tile)) return;
   }
-  // The next tile, in lanes: rows (0: there are no more), q0, k0, first_sees, keys, h.
+  // The next tile, in lanes: rows (0: there are no more), q0, k0, first_sees, keys, h; or
+  // the piece of the line that is worked on.
   volatile int32_t kept;  // (in memory: the loops have no register for it)
   bool first = true;
   const auto find = [&] {
@@ -842,17 +885,16 @@ __global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch
     for (int k = 0; k < 6; ++k) found = lane == k ? told[k] : found;
     kept = found;
   };
-  int64_t place = -1;
   int32_t step0 = 0, step1 = (tile.keys + kKeys - 1) / kKeys;
+  Span span = {};
+  if (w >= 0) span = first_piece<ROWS>(arguments(), w);
   Piece p;
   while (true) {
     if (w >= 0) {
-      const MlaPrefillLaunch b = arguments();
-      const Span s = find_span<ROWS>(b, look_at<ROWS>(b), w, place);
-      if (place >= 0) lds_barrier();  // nobody reads the last piece's keys any more
-      tile = s.tile;
-      step0 = s.step0;
-      step1 = s.step1;
+      kept = in_lanes(span, lane);
+      tile = tile_of<ROWS>(span.r, span.h, span.i);
+      step0 = span.step0;
+      step1 = span.step1;
     }
     attend<W>(
         arguments(), tile, step0, step1, lds, p,
@@ -879,24 +921,24 @@ __global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch
       if (last.rows > 0) write_rows(b, last, p);
       return;
     }
-    // (found again: held beside the loop above, it would cost its registers)
-    asm volatile("" : "+s"(place));
     const MlaPrefillLaunch b = arguments();
-    const Span s = find_span<ROWS>(b, look_at<ROWS>(b), w, place);
-    if (s.begins && s.ends) {
-      write_rows(b, s.tile, p);
+    span = of_lanes(kept);
+    const Tile t = tile_of<ROWS>(span.r, span.h, span.i);
+    if (span.begins && span.ends) {
+      write_rows(b, t, p);
     } else {
-      write_part<W>(b, s.tile, p, 2 * w + (s.begins ? 1 : 0));
-      if (s.begins) {
+      write_part<W>(b, t, p, 2 * w + (span.begins ? 1 : 0));
+      if (span.begins) {
         // the parts of this tile: this one, and one of each worker up to its end
+        const int32_t workers = line_workers(b, Call{span.line, 0});
         int32_t upto = w + 1;
-        while (span_at(s.length, s.workers, upto + 1) < s.tile_end) ++upto;
-        if (threadIdx.x == 0) b.joined[w] = make_int4((int32_t)s.tile.q0, s.tile.rows, s.tile.h, upto - w + 1);
+        while (span_at(span.line * b.heads, workers, upto + 1) < span.tile_end) ++upto;
+        if (threadIdx.x == 0) b.joined[w] = make_int4((int32_t)t.q0, t.rows, t.h, upto - w + 1);
       }
     }
-    wait_vmcnt<0>();  // (the parts' stores, before loads are counted again)
-    place = s.tile_end;
-    if (place >= s.end) return;
+    if (span.tile_end >= span.end) return;
+    next_piece<ROWS>(b, span);
+    lds_barrier();  // nobody reads this piece's keys any more
   }
 }
 
