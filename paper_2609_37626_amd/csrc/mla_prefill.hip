@@ -56,13 +56,19 @@ constexpr int kLoads = 40;                    // loads to LDS a step, by all wav
 constexpr int kAhead = 4;                     // operands read ahead
 constexpr float kMost = 1024.f;               // a lane's eight weights of a row, before the reference moves
 constexpr float kLowest = -1e30f;             // the reference before any score
-constexpr int32_t kTileCost = 1;              // a tile's fixed work, in steps
 // A cut tile's parts pass through memory and a second launch joins them (6 us): tiles of
 // at most kNeverCut steps, 768 keys, do not wait as long, and a worker of the line gets
-// kLeast steps or more.
+// kLeast steps or more.  Places on the line count eighths of a step.  A piece costs 16 to
+// 18 us beside its steps of 2.1 (first loads, the diagonal, writing its part), kTileCost,
+// and a step of a tile of half the rows or less, a wave a SIMD instead of two, 0.65 of
+// others (95 us against 145).  Counted so, 8 heads of 8192 rows take 207 us, 20 of 382 and
+// 512 rows over 18k and 10k keys 192; with every step alike and a tile's cost of one 241
+// and 197.  (Costs of 4 and 12 steps: 211 and 214, 192 and 188.)
 constexpr int32_t kNeverCut = 12;
 constexpr int32_t kLeast = 4;
-constexpr int64_t kLongest = (int64_t)1 << 50;  // a head's line (2^38 for any indptr that does not decrease)
+constexpr int32_t kStep = 8, kHalfStep = 5;
+constexpr int32_t kTileCost = 8 * kStep;
+constexpr int64_t kLongest = (int64_t)1 << 50;  // a head's line (2^41 for any indptr that does not decrease)
 constexpr int kSorted = 4;                    // requests a lane that the order of the blocks looks at
 
 constexpr int kWaveRows = 32;
@@ -125,16 +131,28 @@ template <int ROWS>
 __device__ __forceinline__ int32_t tiles_of(int32_t nq) {
   return (nq + ROWS - 1) / ROWS;
 }
-// Steps that a request's tile i is counted as on the line: its own, at most as many
-// as this, and its fixed work; D i + first(r), D = ROWS / 64.  The line's length up to
-// tile i is i first + D i (i - 1) / 2.
+// A request's tile i on the line: a tile's cost, then base + D i steps, D = ROWS / 64, its
+// own and at most D more.  The line's length up to tile i, of whole tiles all.
 template <int ROWS>
-__device__ __forceinline__ int32_t line_first(const Request& r) {
-  return max(0, (r.nk - r.nq + kKeys - 1) / kKeys) + ROWS / kKeys + kTileCost;
+__device__ __forceinline__ int32_t line_base(const Request& r) {
+  return max(0, (r.nk - r.nq + kKeys - 1) / kKeys) + ROWS / kKeys;
 }
 template <int ROWS>
-__device__ __forceinline__ int64_t line_upto(int64_t i, int32_t first) {
-  return i * (first + ROWS / kKeys / 2 * (i - 1));
+__device__ __forceinline__ int64_t line_upto(int64_t i, int32_t base, int32_t cost) {
+  return i * ((int64_t)kStep * base + cost + kStep * (ROWS / kKeys) / 2 * (i - 1));
+}
+template <int ROWS>
+__device__ __forceinline__ int32_t line_step(const Request& r, int32_t i) {
+  return r.nq - i * ROWS <= ROWS / 2 ? kHalfStep : kStep;
+}
+template <int ROWS>
+__device__ __forceinline__ int64_t line_tile(const Request& r, int32_t i, int32_t cost) {
+  return (int64_t)line_step<ROWS>(r, i) * (line_base<ROWS>(r) + ROWS / kKeys * i) + cost;
+}
+template <int ROWS>
+__device__ __forceinline__ int64_t line_request(const Request& r, int32_t cost) {
+  const int32_t n = tiles_of<ROWS>(r.nq);
+  return n > 0 ? line_upto<ROWS>(n - 1, line_base<ROWS>(r), cost) + line_tile<ROWS>(r, n - 1, cost) : 0;
 }
 
 __device__ __forceinline__ int32_t uniform(int32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
@@ -182,21 +200,23 @@ __device__ __forceinline__ int32_t wave_min(int32_t v) {
 
 // What every workgroup finds out by itself about the whole call.
 struct Call {
-  int64_t line;     // a head's steps
-  int32_t longest;  // the longest tile's
+  int64_t steps;    // a head's, in eighths
+  int32_t tiles;    // a head's
+  int32_t longest;  // the longest tile's steps
 };
 template <int ROWS>
 __device__ __forceinline__ Call look_at(const MlaPrefillLaunch& a) {
   const int lane = threadIdx.x & 63;
-  int64_t line = 0;
+  int64_t steps = 0, tiles = 0;
   int32_t longest = 0;
   for (int32_t b = lane; b < a.B; b += 64) {
     const Request r = request(a, b);
     const int32_t n = tiles_of<ROWS>(r.nq);
-    line += line_upto<ROWS>(n, line_first<ROWS>(r));
+    steps += line_request<ROWS>(r, 0);
+    tiles += n;
     longest = max(longest, n > 0 ? (r.nk + kKeys - 1) / kKeys : 0);
   }
-  return {wave_sum(line), wave_max(longest)};
+  return {wave_sum(steps), (int32_t)min(wave_sum(tiles), (int64_t)INT_MAX), wave_max(longest)};
 }
 
 // Block number `rank` of the requests' blocks of 2^shift tiles, counted from a request's last
@@ -280,13 +300,12 @@ __device__ __forceinline__ bool find_block(const MlaPrefillLaunch& a, int32_t ra
 
 // The tile that holds place `at` of a head's line: its request, which of it, and where it begins.
 template <int ROWS>
-__device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int64_t at, Request& r, int32_t& tile, int64_t& begin) {
+__device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int32_t cost, int64_t at, Request& r, int32_t& tile, int64_t& begin) {
   const int lane = threadIdx.x & 63;
   int64_t behind = 0;
   for (int32_t b0 = 0; b0 < a.B; b0 += 64) {
     const Request mine = request(a, min(b0 + lane, a.B - 1));
-    const int32_t n = b0 + lane < a.B ? tiles_of<ROWS>(mine.nq) : 0;
-    const int64_t own = line_upto<ROWS>(n, line_first<ROWS>(mine)), upto = wave_prefix(own);
+    const int64_t own = b0 + lane < a.B ? line_request<ROWS>(mine, cost) : 0, upto = wave_prefix(own);
     const uint64_t past = __ballot(behind + upto > at);
     if (!past) {
       behind += uniform(upto, 63);
@@ -296,16 +315,16 @@ __device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int64_t at
     r = uniform(mine, who);
     behind += uniform(upto - own, who);
     // the last i with line_upto(i) <= at - behind
-    const int32_t first = line_first<ROWS>(r);
+    const int32_t base = line_base<ROWS>(r);
     const int64_t x = at - behind;
-    constexpr double kD = 0.5 * (ROWS / kKeys);
-    const double half = 0.5 * (first - kD) / kD;
+    constexpr double kD = 0.5 * kStep * (ROWS / kKeys);
+    const double half = 0.5 * ((double)kStep * base + cost - kD) / kD;
     int64_t i = (int64_t)(__builtin_sqrt(half * half + (double)x / kD) - half);
     i = min(max(i, (int64_t)0), (int64_t)tiles_of<ROWS>(r.nq) - 1);
-    while (i > 0 && line_upto<ROWS>(i, first) > x) --i;
-    while (i + 1 < tiles_of<ROWS>(r.nq) && line_upto<ROWS>(i + 1, first) <= x) ++i;
+    while (i > 0 && line_upto<ROWS>(i, base, cost) > x) --i;
+    while (i + 1 < tiles_of<ROWS>(r.nq) && line_upto<ROWS>(i + 1, base, cost) <= x) ++i;
     tile = __builtin_amdgcn_readfirstlane((int32_t)i);
-    begin = behind + line_upto<ROWS>(tile, first);
+    begin = behind + line_upto<ROWS>(tile, base, cost);
     return true;
   }
   return false;
@@ -681,12 +700,13 @@ __device__ __forceinline__ void write_part(const MlaPrefillLaunch& a, const Tile
 
 // Workers of the line: all that fit on the chip, or as many as get kLeast steps.
 __device__ __forceinline__ int32_t line_workers(const MlaPrefillLaunch& a, const Call& call) {
-  const int64_t most = call.line * a.heads / kLeast / 8 * 8;
+  const int64_t most = call.steps * a.heads / (kStep * kLeast) / 8 * 8;
   return (int32_t)min(max(most, (int64_t)8), (int64_t)a.workers);
 }
 // Whether the tiles are cut: where the longest one takes longer than all of them over the chip.
 __device__ __forceinline__ bool is_cut(const MlaPrefillLaunch& a, const Call& call) {
-  return call.longest > kNeverCut && call.line <= kLongest && call.longest * (int64_t)a.workers > call.line * a.heads;
+  return call.longest > kNeverCut && call.steps <= kLongest &&
+         (int64_t)kStep * call.longest * a.workers > (call.steps + (int64_t)kStep * call.tiles) * a.heads;
 }
 
 // Worker w's piece of the line: of tile `i` of a request.
@@ -697,7 +717,8 @@ struct Span {
   Request r;
   int32_t i, h;
   int64_t begin, tile_end, end;  // the tile's place on the line, its end, the worker's end
-  int64_t line;                  // a head's steps
+  int64_t line;                  // a head's
+  int32_t cost, workers;         // a tile's cost on it, and who shares it
   int32_t step0, step1;
   bool begins, ends;  // the piece begins or ends its tile
 };
@@ -705,13 +726,14 @@ struct Span {
 template <int ROWS>
 __device__ __forceinline__ void cut_piece(Span& s, int64_t place) {
   const Tile t = tile_of<ROWS>(s.r, s.h, s.i);
-  s.tile_end = s.begin + line_first<ROWS>(s.r) + ROWS / kKeys * s.i;
-  // the tile's fixed work comes first on the line, and steps that it lacks last
-  const int32_t steps = (t.keys + kKeys - 1) / kKeys;
+  s.tile_end = s.begin + line_tile<ROWS>(s.r, s.i, s.cost);
+  // the tile's cost comes first on the line, and steps that it lacks last
+  const int32_t steps = (t.keys + kKeys - 1) / kKeys, each = line_step<ROWS>(s.r, s.i);
+  const auto step_at = [&](int64_t at) { return min(max((int32_t)(at - s.begin) - s.cost, 0) / each, steps); };
   s.begins = place == s.begin;
   s.ends = s.tile_end <= s.end;
-  s.step0 = min(max((int32_t)(place - s.begin) - kTileCost, 0), steps);
-  s.step1 = s.ends ? steps : min(max((int32_t)(s.end - s.begin) - kTileCost, 0), steps);
+  s.step0 = step_at(place);
+  s.step1 = s.ends ? steps : step_at(s.end);
 }
 template <int ROWS>
 __device__ __forceinline__ void find_piece(const MlaPrefillLaunch& a, Span& s, int64_t place) {
@@ -719,7 +741,7 @@ __device__ __forceinline__ void find_piece(const MlaPrefillLaunch& a, Span& s, i
   s.r = Request{0, 0, 0, 0};
   s.i = 0;
   s.begin = 0;
-  find_place<ROWS>(a, place - s.h * s.line, s.r, s.i, s.begin);
+  find_place<ROWS>(a, s.cost, place - s.h * s.line, s.r, s.i, s.begin);
   s.begin += s.h * s.line;
   cut_piece<ROWS>(s, place);
 }
@@ -727,12 +749,13 @@ __device__ __forceinline__ void find_piece(const MlaPrefillLaunch& a, Span& s, i
 template <int ROWS>
 __device__ __forceinline__ Span first_piece(const MlaPrefillLaunch& a, int32_t w) {
   const Call call = look_at<ROWS>(a);
-  const int32_t workers = line_workers(a, call);
-  const int64_t length = call.line * a.heads;
   Span s;
-  s.line = call.line;
-  s.end = span_at(length, workers, w + 1);
-  find_piece<ROWS>(a, s, span_at(length, workers, w));
+  s.workers = line_workers(a, call);
+  // (not more than a quarter of a worker's steps)
+  s.cost = (int32_t)min((int64_t)kTileCost, call.steps * a.heads / (4 * s.workers));
+  s.line = call.steps + (int64_t)call.tiles * s.cost;
+  s.end = span_at(s.line * a.heads, s.workers, w + 1);
+  find_piece<ROWS>(a, s, span_at(s.line * a.heads, s.workers, w));
   return s;
 }
 template <int ROWS>
@@ -747,12 +770,13 @@ __device__ __forceinline__ void next_piece(const MlaPrefillLaunch& a, Span& s) {
 }
 // What is needed of it behind the loops, in the lanes of one register.
 __device__ __forceinline__ int32_t in_lanes(const Span& s, int lane) {
-  const int32_t told[13] = {s.r.q0, s.r.nq, s.r.k0, s.r.nk, s.i, s.h, (s.begins ? 1 : 0) | (s.ends ? 2 : 0),
+  const int32_t told[15] = {s.r.q0, s.r.nq, s.r.k0, s.r.nk, s.i, s.h, (s.begins ? 1 : 0) | (s.ends ? 2 : 0),
                             (int32_t)s.tile_end, (int32_t)(s.tile_end >> 32), (int32_t)s.end, (int32_t)(s.end >> 32),
-                            (int32_t)s.line, (int32_t)(s.line >> 32)};
+                            (int32_t)s.line, (int32_t)(s.line >> 32),
+                            s.cost, s.workers};
   int32_t v = 0;
 #pragma unroll
-  for (int k = 0; k < 13; ++k) v = lane == k ? told[k] : v;
+  for (int k = 0; k < 15; ++k) v = lane == k ? told[k] : v;
   return v;
 }
 __device__ __forceinline__ Span of_lanes(int32_t v) {
@@ -766,6 +790,8 @@ __device__ __forceinline__ Span of_lanes(int32_t v) {
   s.tile_end = wide(7);
   s.end = wide(9);
   s.line = wide(11);
+  s.cost = uniform(v, 13);
+  s.workers = uniform(v, 14);
   return s;
 }
 
@@ -930,9 +956,8 @@ __global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch
       write_part<W>(b, t, p, 2 * w + (span.begins ? 1 : 0));
       if (span.begins) {
         // the parts of this tile: this one, and one of each worker up to its end
-        const int32_t workers = line_workers(b, Call{span.line, 0});
         int32_t upto = w + 1;
-        while (span_at(span.line * b.heads, workers, upto + 1) < span.tile_end) ++upto;
+        while (span_at(span.line * b.heads, span.workers, upto + 1) < span.tile_end) ++upto;
         if (threadIdx.x == 0) b.joined[w] = make_int4((int32_t)t.q0, t.rows, t.h, upto - w + 1);
       }
     }
@@ -951,14 +976,15 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
   const int32_t row = blockIdx.y * 16 + (threadIdx.x >> 4), lane = threadIdx.x & 15;
   if (record.x < 0 || row >= record.y) return;
   const auto slot = [&](int32_t k) { return ((int64_t)(k == 0 ? 2 * w + 1 : 2 * (w + k)) * ROWS + row); };
-  // (four parts' loads at once; a part without a weight holds zeros)
   float top = kLowest, sum = 0.f;
   f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-  for (int32_t k0 = 0; k0 < record.w; k0 += 4) {
-    f32x2 ml[4];
-    f32x4 v[4][2];
+  // N parts, their loads at once (a part without a weight holds zeros)
+  const auto join = [&](int32_t k0, auto n_) {
+    constexpr int N = decltype(n_)::value;
+    f32x2 ml[N];
+    f32x4 v[N][2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
       const int64_t at = slot(min(k0 + i, record.w - 1));
       ml[i] = *(const f32x2*)(a.part_ml + at * 2);
       v[i][0] = *(const f32x4*)(a.part_out + at * kValue + 8 * lane);
@@ -966,21 +992,24 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
     }
     float to = top;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) to = ml[i][0] > to || ml[i][0] != ml[i][0] ? ml[i][0] : to;
+    for (int i = 0; i < N; ++i) to = ml[i][0] > to || ml[i][0] != ml[i][0] ? ml[i][0] : to;
     const float old = __builtin_amdgcn_exp2f(top - to);
     top = to;
     sum *= old;
     lo *= old;
     hi *= old;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
       if (k0 + i >= record.w) break;
       const float by = __builtin_amdgcn_exp2f(ml[i][0] - to);
       sum += by * ml[i][1];
       lo += by * v[i][0];
       hi += by * v[i][1];
     }
-  }
+  };
+  int32_t k = 0;
+  for (; k + 8 < record.w; k += 16) join(k, std::integral_constant<int, 16>{});
+  for (; k < record.w; k += 4) join(k, std::integral_constant<int, 4>{});
   const int64_t n = (int64_t)(record.x + row) * a.heads + record.z;
   const float by = sum == 0.f ? 0.f : 1.f / sum;
   lo *= by;
