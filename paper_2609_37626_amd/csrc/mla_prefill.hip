@@ -223,13 +223,14 @@ __device__ __forceinline__ Call look_at(const MlaPrefillLaunch& a) {
 // tile, the longest first: which of its request's and of which request (false: none).
 // Block j counts as K - D j steps, K its request's last tile's: how many
 // blocks are longer than a length is a sum over the requests, and the rank's length
-// is found by halving.  Past 64 kSorted requests the blocks go in the requests' order.
+// is found by halving.  Past 64 kSorted requests, and where all tiles begin at once anyway
+// (`sorted` false: 15.1 us for four short prompts, 15.6 sorted), the blocks go in the requests' order.
 template <int ROWS>
-__device__ __forceinline__ bool find_block(const MlaPrefillLaunch& a, int32_t rank, int shift, Request& r, int32_t& block) {
+__device__ __forceinline__ bool find_block(const MlaPrefillLaunch& a, bool sorted, int32_t rank, int shift, Request& r, int32_t& block) {
   const int lane = threadIdx.x & 63;
   constexpr int kLog = ROWS == 256 ? 2 : 1;  // of a tile's steps
   const int D = 1 << (kLog + shift);
-  if (a.B <= 64 * kSorted) {
+  if (sorted && a.B <= 64 * kSorted) {
     Request mine[kSorted];
     int32_t blocks[kSorted], top[kSorted], most = INT_MIN, least = INT_MAX;
 #pragma unroll
@@ -813,7 +814,7 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_order_kernel(MlaPrefillL
     const int32_t rank = (int32_t)blockIdx.x * (kThreads / 64) + wave;
     if (rank >= blocks) return;
     Block b = {};
-    if (!find_block<ROWS>(a, rank, shift, b.r, b.block)) b.r.nq = 0;
+    if (!find_block<ROWS>(a, true, rank, shift, b.r, b.block)) b.r.nq = 0;
     if (lane == 0) to[rank] = b;
     return;
   }
@@ -875,7 +876,7 @@ __global__ __launch_bounds__(64 * W, 2) void mla_prefill_kernel(MlaPrefillLaunch
     Request r;
     int32_t block;
     const int32_t at = blockIdx.x >> 3;
-    if (!find_block<ROWS>(a, (int32_t)rank_of(at), shift, r, block) || !tile_at(at, r, block, tile)) return;
+    if (!find_block<ROWS>(a, gridDim.x > (uint32_t)a.units, (int32_t)rank_of(at), shift, r, block) || !tile_at(at, r, block, tile)) return;
   }
   // The next tile, in lanes: rows (0: there are no more), q0, k0, first_sees, keys, h; or
   // the piece of the line that is worked on.
