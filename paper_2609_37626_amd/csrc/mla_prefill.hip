@@ -1021,7 +1021,7 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
 }
 
 template <int W>
-hipError_t launch_tiles(const MlaPrefillLaunch& a, hipStream_t s) {
+hipError_t launch_tiles(const MlaPrefillLaunch& a, bool small, hipStream_t s) {
   constexpr int kRows = tile_rows(W);
   MlaPrefillLaunch l = a;
   const int32_t workers = (W == 8 ? 1 : 2) * a.units / 8 * 8;
@@ -1034,7 +1034,7 @@ hipError_t launch_tiles(const MlaPrefillLaunch& a, hipStream_t s) {
   int64_t groups = (blocks * a.heads + 7) / 8 * 8 << shift;
   if (a.num_keys <= kNeverCut * kKeys) l.joined = nullptr;
   else groups = max(groups, (int64_t)l.workers);
-  if (groups > l.workers) {
+  if (groups > (small ? 4 : 1) * (int64_t)l.workers) {
     groups = l.workers;
     const int64_t waves = a.B <= 64 * kSorted ? blocks : 1;
     hipLaunchKernelGGL((mla_prefill_order_kernel<kRows>), dim3((unsigned)((waves + kThreads / 64 - 1) / (kThreads / 64))), dim3(kThreads), 0, s,
@@ -1058,7 +1058,12 @@ hipError_t launch_mla_prefill(const MlaPrefillLaunch& a, hipStream_t s) {
   const int64_t rows = max((int64_t)a.num_rows / a.B, (int64_t)1), keys = max((int64_t)a.num_keys / a.B, rows);
   const int64_t steps = (keys - rows / 2) / kKeys, tiles = (rows + 127) / 128 * a.B * a.heads;
   const bool cut = keys > kNeverCut * kKeys && keys / kKeys * 2 * a.units > tiles * steps;
-  return cut || steps >= 40 ? launch_tiles<8>(a, s) : launch_tiles<4>(a, s);
+  if (cut || steps >= 40) return launch_tiles<8>(a, false, s);
+  // A workgroup each for a few short tiles: they are over before the order's launch is made
+  // up for (us, a workgroup each / one after the other: 32 heads of 34 x 18 rows 26.8 / 30.3,
+  // 16 of 64 x 250 96 / 103, 8 of 100 x 60 32 / 36; but 128 of 64 x 8 130 / 123, 64 of
+  // 10 x 500 151 / 143).
+  return launch_tiles<4>(a, keys < 384, s);
 }
 
 }  // namespace splash

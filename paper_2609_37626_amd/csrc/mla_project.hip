@@ -36,8 +36,14 @@ __device__ __forceinline__ u32x4 round8(f32x4 lo, f32x4 hi) {
 }
 
 // Workgroups go round the 8 XCDs: `inner` neighbours of one item share one of them, one
-// after the other.  The items' places; false past the last.
+// after the other; fewer than 8 items are spread over all.  The items' places; false past
+// the last.
 __device__ __forceinline__ bool place(uint32_t at, uint32_t items, uint32_t inner, uint32_t& item, uint32_t& part) {
+  if (items < 8) {
+    item = at % items;
+    part = at / items;
+    return part < inner;
+  }
   const uint32_t xcd = at & 7, n = at >> 3;
   part = n % inner;
   item = n / inner * 8 + xcd;
@@ -192,26 +198,26 @@ __global__ __launch_bounds__(kThreads, 2) void mla_absorb_kernel(MlaAbsorbLaunch
   wait_vmcnt<0>();
 }
 
-// A head for 128 tokens.  Waves w and w + 4 take 128 of the 512 latent columns, 64 tokens
-// each, so that each row is read by one wave once; the four slices' sums meet in LDS, 32
+// A head for 32 TILES tokens.  Waves w and w + 4 take 128 of the 512 latent columns, half
+// of the tokens each, so that each row is read by one wave once; the four slices' sums meet in LDS, 32
 // values a wave.  The weight comes through LDS in whole lines, 256 bytes of a row to a
 // slice, in chunks of 16 bytes at chunk ^ (row & 15).
 constexpr int kSlices = 4;
 constexpr int kSlice = kDimV / kSlices;
 constexpr int kExpandWaves = 2 * kSlices;
-constexpr int kExpandTiles = 4;  // tiles of a wave, all on their way at once
-constexpr int kExpandChunk = 2 * kTile * kExpandTiles;
+template <int TILES>  // of a wave, all on their way at once
 __global__ __launch_bounds__(64 * kExpandWaves, 2) void mla_expand_kernel(MlaExpandLaunch a) {
   typedef float Sums[kExpandWaves][kTile][kValue + 4];
   __shared__ __align__(16) uint8_t lds[2 * sizeof(Sums)];
   static_assert(sizeof(lds) >= kValue * kDimV * 2, "the weight");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4, slice = wave % kSlices, side = wave / kSlices;
+  constexpr int kSide = kTile * TILES;
   uint32_t h, part;
-  if (!place(blockIdx.x, a.heads, ((uint32_t)a.num_tokens + kExpandChunk - 1) / kExpandChunk, h, part)) return;
-  const int64_t first = (int64_t)part * kExpandChunk;
-  const int64_t begin = min(first + side * (kExpandChunk / 2), (int64_t)a.num_tokens);
-  const int64_t end = min(begin + kExpandChunk / 2, (int64_t)a.num_tokens);
+  if (!place(blockIdx.x, a.heads, ((uint32_t)a.num_tokens + 2 * kSide - 1) / (2 * kSide), h, part)) return;
+  const int64_t first = (int64_t)part * 2 * kSide;
+  const int64_t begin = min(first + side * kSide, (int64_t)a.num_tokens);
+  const int64_t end = min(begin + kSide, (int64_t)a.num_tokens);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_AS uint8_t*)lds;
   const uint16_t* w = a.w + h * a.w_head + kSlice * slice;
   const int row = lane >> 4, slot = lane & 15;  // of a load's four rows
@@ -221,9 +227,9 @@ __global__ __launch_bounds__(64 * kExpandWaves, 2) void mla_expand_kernel(MlaExp
     load_lds_from(w + v * a.w_row + 8 * (slot ^ (v & 15)), lds0 + (slice * kValue + v - row) * kRowBytes);
   }
   const uint16_t* x = a.x + (int64_t)h * kDimV + kSlice * slice + 8 * g;
-  bf16x8 xf[kExpandTiles][4];
+  bf16x8 xf[TILES][4];
 #pragma unroll
-  for (int t = 0; t < kExpandTiles; ++t)
+  for (int t = 0; t < TILES; ++t)
     if (begin + kTile * t < end)
 #pragma unroll
       for (int k = 0; k < 4; ++k) xf[t][k] = load8(x + min(begin + kTile * t + c, end - 1) * a.heads * kDimV + 32 * k);
@@ -238,7 +244,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, 2) void mla_expand_kernel(MlaExp
   lds_barrier();  // the weight's place becomes the sums'
   Sums* sums = (Sums*)lds;
 #pragma unroll
-  for (int t = 0; t < kExpandTiles; ++t) {
+  for (int t = 0; t < TILES; ++t) {
     if (first + kTile * t >= a.num_tokens) break;  // (of the first side: the same for all waves)
     const int64_t n0 = begin + kTile * t;
     if (n0 < end) {
@@ -280,10 +286,21 @@ hipError_t launch_mla_absorb(const MlaAbsorbLaunch& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_mla_expand(const MlaExpandLaunch& a, hipStream_t s) {
-  const uint32_t chunks = ((uint32_t)a.num_tokens + kExpandChunk - 1) / kExpandChunk;
-  hipLaunchKernelGGL(mla_expand_kernel, dim3(((uint32_t)a.heads + 7) / 8 * 8 * chunks), dim3(64 * kExpandWaves), 0, s, a);
+namespace {
+template <int TILES>
+hipError_t launch_expand(const MlaExpandLaunch& a, hipStream_t s) {
+  const uint32_t chunks = ((uint32_t)a.num_tokens + 2 * kTile * TILES - 1) / (2 * kTile * TILES);
+  hipLaunchKernelGGL((mla_expand_kernel<TILES>), dim3(((uint32_t)a.heads + 7) / 8 * 8 * chunks), dim3(64 * kExpandWaves), 0, s, a);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t launch_mla_expand(const MlaExpandLaunch& a, hipStream_t s) {
+  // The fewest tokens a workgroup (32, 64 or 128) with which all of them begin at once, one
+  // a compute unit: 635 tokens of 8 heads take 7.5 us so, 11.1 at 128.
+  const auto groups = [&](int64_t tokens) { return a.heads * ((a.num_tokens + tokens - 1) / tokens); };
+  if (groups(32) <= 256) return launch_expand<1>(a, s);
+  return groups(64) <= 256 ? launch_expand<2>(a, s) : launch_expand<4>(a, s);
 }
 
 }  // namespace splash
