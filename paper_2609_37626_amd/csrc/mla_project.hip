@@ -134,9 +134,15 @@ __global__ __launch_bounds__(kThreads, 2) void mla_absorb_kernel(MlaAbsorbLaunch
     return;
   }
   const uint32_t chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
+  // A head's four blocks on one XCD, which then reads its queries once (256 tokens of 128
+  // heads: 15.0 us, 16.4 with the blocks apart), where the heads fill the XCDs evenly.
+  constexpr uint32_t kColumnBlocks = kDimV / kColumns;
+  const bool even = a.heads % 8 == 0;
   uint32_t item, part;
-  if (!place(blockIdx.x, (uint32_t)a.heads * (kDimV / kColumns), chunks, item, part)) return;
-  const int c = lane & 15, g = lane >> 4, h = item / (kDimV / kColumns), block = item % (kDimV / kColumns);
+  if (!place(blockIdx.x, even ? a.heads : a.heads * kColumnBlocks, even ? chunks * kColumnBlocks : chunks, item, part)) return;
+  const int c = lane & 15, g = lane >> 4, h = even ? item : item / kColumnBlocks;
+  const int block = (even ? part : item) % kColumnBlocks;
+  if (even) part /= kColumnBlocks;
   const int64_t begin = (int64_t)part * chunk, end = min(begin + chunk, (int64_t)a.num_tokens);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(LDS_AS uint8_t*)lds;
   const int row = lane >> 4, slot = lane & 15;  // of a load's four rows

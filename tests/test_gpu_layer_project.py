@@ -92,6 +92,12 @@ def test_expand(n, h):
     check_expand(n, h, seed=n + h)
 
 
+@pytest.mark.parametrize("n,h", [(33, 128), (64, 130), (129, 129), (700, 20), (650, 40), (4100, 1), (1025, 7)])
+def test_expand_of_more_tokens(n, h):
+    """32, 64 and 128 tokens a workgroup, heads fewer and more than the XCDs."""
+    check_expand(n, h, seed=n + h)
+
+
 def test_expand_views():
     check_expand(37, 5, wide=True, seed=1)
 

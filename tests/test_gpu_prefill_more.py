@@ -28,11 +28,13 @@ def test_more_tiles_than_workgroups_in_the_requests_order():
     rng = rng_of(31)
     p = Prompts(rng.integers(0, 4, 400), rng.integers(0, 30, 400), 4, seed=32)
     some_heads(p, [0, 1, 2, 3], "400 short prompts")
+    some_heads(Prompts(rng.integers(0, 4, 400), rng.integers(0, 30, 400), 20, seed=39), [0, 19], "400 short prompts, 20 heads")
     p = Prompts([700, 0, 300] + [1] * 270, [0, 5, 900] + [3] * 270, 40, seed=33)
     some_heads(p, [0, 39], "two long prompts before 270 tokens")
 
 
 @pytest.mark.parametrize("new,old,heads", [([130] * 9, [0, 7, 64, 100, 31, 500, 1, 2, 3], 40), ([390, 20, 650], [0, 0, 0], 64),
+                                           ([500, 420, 610], [0, 30, 0], 64), ([18] * 34, [0] * 34, 32),
                                            ([515, 510], [3000, 2950], 56), ([300, 700], [4100, 3300], 56)])
 def test_more_tiles_than_workgroups(new, old, heads):
     """Both tile widths, last tiles that are not full, groups that are not."""
