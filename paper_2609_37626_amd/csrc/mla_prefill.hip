@@ -20,7 +20,7 @@
 //
 // Bound: matrix instructions, 320 multiplications and additions each a row and key of a
 // head (192 + 128), at 1.36 PFLOP/s of a large library product.  128 heads of one prompt
-// of 4096 rows: 703 us, 978 TFLOP/s; 32 of 2 x 4096 rows over 4096 more: 889 us, 1,160.
+// of 4096 rows: 697 us, 986 TFLOP/s; 32 of 2 x 4096 rows over 4096 more: 889 us, 1,160.
 // Of the first, the matrix instructions alone take 420 us, the loads into LDS 130, its
 // reads 100 and the softmax 80 that two waves a SIMD do not hide; a tile costs 8 us beside
 // its turns (loads of its first step and queries 3.4, writing the last one's rows 3.6, the
