@@ -8,7 +8,9 @@
 //       16 t + 4 g + i of row c: the weights of a row stay in its four lanes.
 //   PV  O^T[value, row] = V^T P^T.  The product's slot (g, j) is key 4 g + j of tile 0
 //       (j < 4) or 4 g + j - 4 of tile 1: P goes from QK's result to PV's operand in the
-//       lane that has it, and V's transposing reads take the rows in that order.
+//       lane that has it, and V's transposing reads take the rows in that order.  P is
+//       rounded to bf16, V's type, for it (outputs are off by 2.1e-3 of their norm, 1.6e-3
+//       with exact weights); the weights' sum is of the unrounded ones.
 // A turn multiplies QK of its keys while the exponentials of the last turn's scores are
 // dealt out between the matrix instructions, then PV of the last turn: a step's values
 // are the second half of the step before and the first of its own.
