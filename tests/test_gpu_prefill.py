@@ -49,7 +49,7 @@ def test_few_rows_over_a_long_history(heads):
 
 
 @pytest.mark.parametrize("new,old,heads", [([800], [0], 80), ([1000, 1100, 7], [0, 30, 0], 40), ([520, 900], [4000, 10], 2),
-                                           ([1, 300, 4096], [0, 0, 0], 24), ([256, 257, 255], [6000, 6000, 6001], 3)])
+                                           ([1, 300, 4096], [0, 0, 0], 25), ([256, 257, 255], [6000, 6000, 6001], 3)])
 def test_tiles_whole_and_cut(new, old, heads):
     """Long and short tiles in both widths, whole and over several workgroups: some heads against the oracle."""
     p = Prompts(new, old, heads, seed=sum(new))

@@ -47,7 +47,7 @@ def gather(d, pages=FAKE, table=FAKE, begin=FAKE, indptr=FAKE, rows=4, latent=FA
     return B.lib().splash_mla_gather(pages, table, begin, indptr, rows, latent, ls, key, ks, None if d is None else d, None)
 
 
-def absorb(q=FAKE, qt=16 * 192, qh=192, w=FAKE, wh=256 * 512, wr=512, pos=FAKE, ps=4, rope=None, n=4, heads=20, out=2 * FAKE):
+def absorb(q=FAKE, qt=20 * 192, qh=192, w=FAKE, wh=256 * 512, wr=512, pos=FAKE, ps=4, rope=None, n=4, heads=20, out=2 * FAKE):
     return B.lib().splash_mla_absorb_q(q, qt, qh, w, wh, wr, pos, ps, rope, n, heads, out, None)
 
 
