@@ -333,6 +333,12 @@ __device__ __forceinline__ bool find_place(const MlaPrefillLaunch& a, int32_t co
   return false;
 }
 
+// A row's sum over its four lanes.
+__device__ __forceinline__ float row_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
 // Softmax and products of a tile's steps [step0, step1) in this workgroup's waves;
 // `before` runs once the first loads are on their way (p still holds the last tile),
 // `after` once the wave has multiplied all that it sees, while others still do.
@@ -626,22 +632,68 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
   } else {
     after();
   }
-  if (__any(odd)) {
-    // (the first turn's values, and from the last turn without masks on)
-    const int32_t first = step0 * kKeys, to = min(mine * kHalf, tile.keys);
+  // Values that are not finite: the masked turns' products do not have them, and where an
+  // infinity met a weight that is 0 in fp32 alone (a score far below the reference, or a
+  // reference that moved far later on) the others' are NaN.  A sum that is not finite,
+  // unless by its row's scores, is made anew of all such values that the row sees, as they
+  // are: an infinity stays one, both signs or a NaN are NaN.  (32 heads of 4096 rows: 202 us
+  // with or without the look at the sums, 693 where one value of the first key is infinite.)
+  float beyond[R] = {};  // NaN: a sum of the row is not finite
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int d = 0; d < 8; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) beyond[r] = __builtin_fmaf(o[d][r][i], 0.f, beyond[r]);
+  if (__any(odd || beyond[0] != beyond[0] || beyond[1] != beyond[1])) {
+    constexpr float kMax = __FLT_MAX__;  // in place of a sum until its infinity is found
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float l = row_sum(sum[r]);
+      odd |= beyond[r] != beyond[r] && l == l;
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][r][i] = __builtin_fabsf(o[d][r][i]) <= kMax ? o[d][r][i] : copysignf(kMax, o[d][r][i]);
+    }
+    const auto value = [&](int32_t j, int d) { return *(const u32x2*)(v_base + (int64_t)j * a.v_token * 2 + 32 * d + 8 * g); };
+    const int32_t to = __any(odd) ? min(mine * kHalf, tile.keys) : 0;
+    // sixteen keys at a time are looked at, one a lane c
 #pragma unroll 1
-    for (int32_t j = first; j < to; j = j + 1 == first + kHalf ? max(first + kHalf, (2 * full - 1) * kHalf) : j + 1)
+    for (int32_t j0 = step0 * kKeys; j0 < to; j0 += 16) {
+      bool has = false;
 #pragma unroll
       for (int d = 0; d < 8; ++d) {
-        const u32x2 v = *(const u32x2*)(v_base + (int64_t)j * a.v_token * 2 + 32 * d + 8 * g);
+        const u32x2 v = value(min(j0 + c, to - 1), d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t bits = i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16;
+        for (int i = 0; i < 2; ++i) has |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
+      }
+      const uint64_t lanes = __ballot(has);
+      uint32_t keys = (uint32_t)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu;
+#pragma unroll 1
+      for (; keys; keys &= keys - 1) {
+        const int32_t j = j0 + __builtin_ctz(keys);
+        if (j >= to) break;
 #pragma unroll
-          for (int r = 0; r < R; ++r)
-            if ((bits & 0x7f800000u) == 0x7f800000u && j < sees0 + 16 * r + c) o[d][r][i] += __builtin_bit_cast(float, bits);
+        for (int d = 0; d < 8; ++d) {
+          const u32x2 v = value(j, d);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              if ((bits & 0x7f800000u) == 0x7f800000u && j < sees0 + 16 * r + c) o[d][r][i] += __builtin_bit_cast(float, bits);
+          }
         }
       }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)  // (no infinity: finite products past fp32's range)
+          if (__builtin_fabsf(o[d][r][i]) == kMax) o[d][r][i] = copysignf(INFINITY, o[d][r][i]);
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -652,11 +704,6 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
   }
 }
 
-// A row's sum over its four lanes.
-__device__ __forceinline__ float row_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
-}
 __device__ __forceinline__ void write_rows(const MlaPrefillLaunch& a, const Tile& tile, const Piece& p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4;
@@ -981,6 +1028,12 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
   const auto slot = [&](int32_t k) { return ((int64_t)(k == 0 ? 2 * w + 1 : 2 * (w + k)) * ROWS + row); };
   float top = kLowest, sum = 0.f;
   f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+  // (an infinite sum stays one where its part's weight is 0 in fp32)
+  const auto weighed = [](f32x4 x, float by) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __builtin_fabsf(x[i]) == INFINITY ? x[i] : x[i] * by;
+    return x;
+  };
   // N parts, their loads at once (a part without a weight holds zeros)
   const auto join = [&](int32_t k0, auto n_) {
     constexpr int N = decltype(n_)::value;
@@ -999,21 +1052,22 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
     const float old = __builtin_amdgcn_exp2f(top - to);
     top = to;
     sum *= old;
-    lo *= old;
-    hi *= old;
+    lo = weighed(lo, old);
+    hi = weighed(hi, old);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (k0 + i >= record.w) break;
       const float by = __builtin_amdgcn_exp2f(ml[i][0] - to);
       sum += by * ml[i][1];
-      lo += by * v[i][0];
-      hi += by * v[i][1];
+      lo += weighed(v[i][0], by);
+      hi += weighed(v[i][1], by);
     }
   };
   int32_t k = 0;
   for (; k + 8 < record.w; k += 16) join(k, std::integral_constant<int, 16>{});
   for (; k < record.w; k += 4) join(k, std::integral_constant<int, 4>{});
   const int64_t n = (int64_t)(record.x + row) * a.heads + record.z;
+  if (sum == 0.f) lo = hi = (f32x4){0.f, 0.f, 0.f, 0.f};
   const float by = sum == 0.f ? 0.f : 1.f / sum;
   lo *= by;
   hi *= by;
