@@ -16,8 +16,10 @@
 // are the second half of the step before and the first of its own.
 //
 // The softmax runs over the keys once with a reference that moves only where a lane's
-// eight weights of a row pass 1024: below that no sum can overflow, and the lane needs no
-// maximum and no exchange for it, only the sum that it makes anyway.  Each row decides by
+// eight weights of a row pass 1024: below that no sum of weights can overflow, and the lane
+// needs no maximum and no exchange for it, only the sum that it makes anyway.  A row's nk
+// weights are 128 nk at most together (32 of the first turn, 4096 of each other one), so
+// that values up to 2^120 / nk stay in fp32's range.  Each row decides by
 // its own scores, so that its result does not depend on its neighbours.
 //
 // Bound: matrix instructions, 320 multiplications and additions each a row and key of a

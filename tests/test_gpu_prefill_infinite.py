@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2609_37626_amd import binding as B
-from tests.layer_inputs import dev
+from tests.layer_inputs import Prompts, assert_prefill, dev
 
 pytestmark = pytest.mark.gpu
 INF, NAN = float("inf"), float("nan")
@@ -189,3 +189,21 @@ def test_rows_that_see_no_key_in_long_calls(new, old, heads):
             assert bool(((out[n].double().cpu() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -10) * mass).all()), (b, n)
             # lse: 198 roundings of a score's magnitudes, below 2^6
             assert bool(((lse[n].double().cpu() - torch.logsumexp(z, 0)).abs() <= 198 * 2.0 ** -18 + 2.0 ** -10).all())
+
+
+@pytest.mark.parametrize("new,old,heads", [([200], [824], 2), ([40], [6000], 1), ([1024], [4096], 72)])
+def test_values_at_the_end_of_the_range(new, old, heads):
+    """Values of 2^120 / nk and weights that come close to 128 each: all scores behind the first 32 keys 6.8 powers of two
+    above theirs, which moves no reference."""
+    p = Prompts(new, old, heads, seed=6)
+    keys, ones = int(p.keys[0]), np.uint16(0x3F80)
+    p.q[:], p.kv[..., :128], p.key[:] = 0, 0, 0
+    p.q[..., 0] = ones
+    p.scale = np.float32(6.8 * np.log(2.0))
+    p.kv[32:, :, 0] = ones
+    p.kv[..., 128:] = (p.kv[..., 128:] & 0x8000) + ((127 + 120 - int(np.ceil(np.log2(keys)))) << 7)
+    p.kv[..., 128:160] &= 0x7FFF      # sums of one sign
+    out, lse = p.run()
+    some = sorted({0, heads - 1})
+    p.q, p.kv, p.heads = p.q[:, some], p.kv[:, some], len(some)
+    assert_prefill(out[:, some], lse[:, some], p.oracle(), keys, f"{new} over {old}, {heads} heads")
