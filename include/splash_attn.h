@@ -582,7 +582,8 @@ int splash_gqa_attend(const void* q, const void* k_pages, const void* v_pages, c
  *
  * These calls stay inside their buffers whatever the device data holds, and can
  * be captured in a graph.  They need no workspace but splash_mla_prefill's.
- * Strides count elements; `stream` and statuses as above.
+ * Strides count elements (over one token, row, key or head they are not looked at);
+ * `stream` and statuses as above.
  */
 #define SPLASH_DIM_NOPE   128
 #define SPLASH_DIM_ROPE   64

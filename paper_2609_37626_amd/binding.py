@@ -655,9 +655,8 @@ def splash_mla_append(latent, key, slots, kv_pages, kv_scales, desc: MlaDesc, no
         _refuse_pool(desc, dev, kv_pages, slots=(slots, (_I32T,), (n,)), norm_weight=(norm_weight, (_BF16T,), (512,)),
                      kv_scales=(kv_scales if fp8 else None, (_F32T,), (pages, 64)))
     at, stride = _NO_TURN if rope is None else _turn_args(positions, rope, n, dev)
-    # (of one row the stride may be anything)
     _on_device(dev, lib().splash_mla_append, (
-        latent.data_ptr(), ls[0] if n > 1 else 512, key.data_ptr(), ks[0] if n > 1 else 64, None if norm_weight is None else norm_weight.data_ptr(), norm_eps,
+        latent.data_ptr(), ls[0], key.data_ptr(), ks[0], None if norm_weight is None else norm_weight.data_ptr(), norm_eps,
         at, stride, rope, slots.data_ptr(), n, kv_pages.data_ptr(), kv_scales.data_ptr() if fp8 else None, desc), stream)
 
 
@@ -683,11 +682,9 @@ def splash_mla_gather(kv_pages, block_table, row_indptr, latent_out, key_out, de
         _refuse_views(dev, latent_out=(latent_out, (rows, 512)), key_out=(key_out, (rows, 64)))
         _refuse_pool(desc, dev, kv_pages, block_table=(block_table, i32, table), row_indptr=(row_indptr, i32, (b + 1,)),
                      key_begin=(key_begin, i32, (b,)))
-    # (of one row the stride may be anything)
     _on_device(dev, lib().splash_mla_gather, (
         kv_pages.data_ptr(), block_table.data_ptr(), None if key_begin is None else key_begin.data_ptr(),
-        row_indptr.data_ptr(), rows, latent_out.data_ptr(), ls[0] if rows > 1 else 512, key_out.data_ptr(),
-        ks[0] if rows > 1 else 64, desc), stream)
+        row_indptr.data_ptr(), rows, latent_out.data_ptr(), ls[0], key_out.data_ptr(), ks[0], desc), stream)
 
 
 def splash_mla_absorb_q(q, w_uk, q_out, positions=None, rope: Optional[RopeDesc] = None, stream=None) -> None:

@@ -28,6 +28,10 @@ constexpr int64_t kMaxTiles = 1 << 21;
 static_assert(kMaxTiles * kPrefillBlock <= 2 * (int64_t)kPrefillParts * kValue * 4, "every block's place in the workspace");
 constexpr int64_t kMaxTokenStride = 1 << 24;  // 64 rows' byte offsets fit 32 bits
 
+// A stride over `count` items; over one, which nothing walks (a view may report anything
+// there), `none`.
+int64_t walked(int32_t count, int64_t stride, int64_t none = 0) { return count > 1 ? stride : none; }
+
 // The pool's limits beyond validate_mla_desc, and its pages.
 int check_pool(const splash_mla_desc* d, const void* kv_pages) {
   if (d->num_pages > kMaxPoolPages)
@@ -101,6 +105,8 @@ int splash_mla_append(const void* latent, int64_t latent_stride, const void* key
                       float* kv_scales, const splash_mla_desc* desc, void* stream) {
   int st = validate_mla_desc(desc, 1);
   if (st != SPLASH_OK) return st;
+  latent_stride = walked(num_tokens, latent_stride);
+  key_stride = walked(num_tokens, key_stride);
   if (num_tokens < 0 || latent_stride < 0 || key_stride < 0)
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "num_tokens and strides must be >= 0");
   if (num_tokens > kMaxRows) return fail(SPLASH_ERR_UNSUPPORTED, "num_tokens must be at most 2^25 (got %d)", num_tokens);
@@ -139,6 +145,8 @@ int splash_mla_gather(const void* kv_pages, const int32_t* block_table, const in
                       void* key_out, int64_t key_stride, const splash_mla_desc* desc, void* stream) {
   int st = validate_mla_desc(desc, 1);
   if (st != SPLASH_OK) return st;
+  latent_stride = walked(max_rows, latent_stride, kDimV);
+  key_stride = walked(max_rows, key_stride, kRope);
   if (max_rows < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "max_rows < 0");
   if (max_rows > kMaxRows) return fail(SPLASH_ERR_UNSUPPORTED, "max_rows must be at most 2^25 (got %d)", max_rows);
   if (desc->max_pages_per_seq > INT32_MAX / kPage)
@@ -163,6 +171,9 @@ int splash_mla_gather(const void* kv_pages, const int32_t* block_table, const in
 int splash_mla_absorb_q(const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* w_uk,
                         int64_t w_head_stride, int64_t w_row_stride, const int32_t* positions, int64_t position_stride,
                         const splash_rope_desc* rope, int32_t num_tokens, int32_t num_heads, void* q_out, void* stream) {
+  q_token_stride = walked(num_tokens, q_token_stride);
+  q_head_stride = walked(num_heads, q_head_stride);
+  w_head_stride = walked(num_heads, w_head_stride);
   if (num_tokens < 0 || num_heads < 0 || q_token_stride < 0 || q_head_stride < 0)
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "counts and strides must be >= 0");
   if (num_tokens == 0 || num_heads == 0) return SPLASH_OK;
@@ -190,6 +201,9 @@ int splash_mla_absorb_q(const void* q, int64_t q_token_stride, int64_t q_head_st
 int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stride, int64_t w_row_stride,
                           int32_t num_tokens, int32_t num_heads, void* y, int64_t y_token_stride, int64_t y_head_stride,
                           void* stream) {
+  w_head_stride = walked(num_heads, w_head_stride);
+  y_token_stride = walked(num_tokens, y_token_stride);
+  y_head_stride = walked(num_heads, y_head_stride);
   if (num_tokens < 0 || num_heads < 0 || y_token_stride < 0 || y_head_stride < 0)
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "counts and strides must be >= 0");
   if (num_tokens == 0 || num_heads == 0) return SPLASH_OK;
@@ -222,14 +236,18 @@ int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const
                        int32_t num_rows, int32_t num_keys, int32_t num_heads, float softmax_scale, void* out, float* lse,
                        void* workspace, size_t ws_bytes, void* stream) {
   if (!q || !k || !v) return fail(SPLASH_ERR_INVALID_ARGUMENT, "q, k and v must be non-NULL");
+  const auto view = [&](const splash_mla_rows* r, int32_t count) {
+    return splash_mla_rows{r->x, walked(count, r->token_stride), walked(num_heads, r->head_stride)};
+  };
+  const splash_mla_rows views[] = {view(q, num_rows), view(k, num_keys), view(v, num_keys)};
+  key_stride = walked(num_keys, key_stride);
   if (batch < 0 || num_rows < 0 || num_keys < 0 || num_heads < 0 || key_stride < 0)
     return fail(SPLASH_ERR_INVALID_ARGUMENT, "counts and strides must be >= 0");
-  const splash_mla_rows* views[] = {q, k, v};
-  for (const splash_mla_rows* r : views) {
-    if (r->token_stride < 0 || r->head_stride < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "negative stride");
-    if (r->token_stride % 8 || r->head_stride % 8 || !aligned(r->x, 16))
+  for (const splash_mla_rows& r : views) {
+    if (r.token_stride < 0 || r.head_stride < 0) return fail(SPLASH_ERR_INVALID_ARGUMENT, "negative stride");
+    if (r.token_stride % 8 || r.head_stride % 8 || !aligned(r.x, 16))
       return fail(SPLASH_ERR_MISALIGNED, "q, k and v must be 16-byte aligned, with strides of whole 8 elements");
-    if (r->token_stride > kMaxTokenStride) return fail(SPLASH_ERR_UNSUPPORTED, "a token stride past 2^24");
+    if (r.token_stride > kMaxTokenStride) return fail(SPLASH_ERR_UNSUPPORTED, "a token stride past 2^24");
   }
   if (key_stride > kMaxTokenStride) return fail(SPLASH_ERR_UNSUPPORTED, "a token stride past 2^24");
   if (key_stride % 8 || !aligned(key, 16) || !aligned(out, 16) || !aligned(workspace, 16))
@@ -257,13 +275,13 @@ int splash_mla_prefill(const splash_mla_rows* q, const splash_mla_rows* k, const
   a.k = static_cast<const uint16_t*>(k->x);
   a.key = static_cast<const uint16_t*>(key);
   a.v = static_cast<const uint16_t*>(v->x);
-  a.q_token = q->token_stride;
-  a.q_head = q->head_stride;
-  a.k_token = k->token_stride;
-  a.k_head = k->head_stride;
+  a.q_token = views[0].token_stride;
+  a.q_head = views[0].head_stride;
+  a.k_token = views[1].token_stride;
+  a.k_head = views[1].head_stride;
   a.key_token = key_stride;
-  a.v_token = v->token_stride;
-  a.v_head = v->head_stride;
+  a.v_token = views[2].token_stride;
+  a.v_head = views[2].head_stride;
   a.q_indptr = q_indptr;
   a.kv_indptr = kv_indptr;
   a.B = batch;
