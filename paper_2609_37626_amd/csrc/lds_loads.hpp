@@ -20,7 +20,11 @@ __device__ __forceinline__ void lds_barrier() {
 }
 // 16 bytes a lane from base + offset + ADD straight to LDS at `lds` + 16 * lane.  Through
 // asm, so that the compiler does not wait for it at every LDS read; the kernel does.  (The
-// instruction's own offset moves the LDS address as well: M0 is set that much lower.)
+// instruction's own offset moves the LDS address as well: M0 is set that much lower.  M0 is a
+// reserved register: the compiler allocates nothing to it, writes it only for an
+// instruction that takes it, and refuses it as a clobber.  It is not restored: nothing else
+// in the kernels that include this takes it, which their listings show as no mention of m0
+// but these.)
 template <int ADD>
 __device__ __forceinline__ void load_lds(const void* from, uint32_t offset, uint32_t to) {
   const uint64_t at = (uint64_t)from;
