@@ -19,8 +19,9 @@
 // eight weights of a row pass 1024: below that no sum of weights can overflow, and the lane
 // needs no maximum and no exchange for it, only the sum that it makes anyway.  A row's nk
 // weights are 128 nk at most together (32 of the first turn, 4096 of each other one), so
-// that values up to 2^120 / nk stay in fp32's range.  Each row decides by
-// its own scores, so that its result does not depend on its neighbours.
+// that values up to 2^120 / nk stay in fp32's range.  Each row decides by its own scores:
+// other rows' values do not reach its result (their lengths do, where tiles are cut: the
+// cuts' places are the whole call's, and the order of a row's sums with them).
 //
 // Bound: matrix instructions, 320 multiplications and additions each a row and key of a
 // head (192 + 128), at 1.36 PFLOP/s of a large library product.  128 heads of one prompt
