@@ -697,7 +697,8 @@ int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stri
  *   out   bf16 [num_rows, num_heads, 128] (round to nearest even), over none of the
  *         inputs
  *   lse   fp32 [num_rows, num_heads]; may be NULL
- *   workspace   splash_mla_prefill_workspace_size bytes, 16-byte aligned; it holds
+ *   workspace   splash_mla_prefill_workspace_size bytes (68 MB whatever the sizes: two
+ *         parts of a tile for each workgroup of the chip), 16-byte aligned; it holds
  *         what one call leaves for its own second launch, and calls that may overlap
  *         take one each
  * Products are summed in fp32; a weight is rounded to bf16 where it meets V (2^-8), its

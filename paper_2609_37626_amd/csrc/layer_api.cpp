@@ -21,9 +21,12 @@ constexpr int32_t kMaxPoolPages = 1 << 25;  // a slot (64 * page + place) fits i
 constexpr int32_t kMaxRows = 1 << 25;       // a launch holds less than 2^32 lanes: 64 a row
 constexpr int32_t kMaxProjected = 1 << 24;  // tokens, 16 of them a tile
 constexpr int32_t kMaxLayerHeads = 1024;
-// A launch holds less than 2^32 lanes: at most 8 a row and head of a projection, 512 a
-// tile of 128 rows (and its padding) of a prompt.
+// A launch holds less than 2^32 lanes: at most 8 a row and head of a projection.
 constexpr int64_t kMaxProjectedRows = 1 << 28;
+// Tiles of a prompt, of all heads.  Its launches take no more workgroups than stay on the
+// chip (a few each where tiles are short), so that two smaller things have to fit: a block of
+// the order for the tiles of one head, in the parts' place, and an int32 for each place on an
+// XCD.  The limit leaves room for both.
 constexpr int64_t kMaxTiles = 1 << 21;
 static_assert(kMaxTiles * kPrefillBlock <= 2 * (int64_t)kPrefillParts * kValue * 4, "every block's place in the workspace");
 constexpr int64_t kMaxTokenStride = 1 << 24;  // 64 rows' byte offsets fit 32 bits
@@ -82,6 +85,7 @@ int check_projection(int32_t num_tokens, int32_t num_heads, const void* w, int64
   return SPLASH_OK;
 }
 
+// The same for every call: parts of all workers (whose number is the chip's), 68 MB.
 struct PrefillLayout {
   size_t joined, part_ml, part_out, total;  // the tickets come first
 };
