@@ -21,6 +21,7 @@
 
 #include "device_types.hpp"
 #include "layer.hpp"
+#include "quotient.hpp"
 #include "splash_attn.h"
 #include "turn.hpp"
 
@@ -90,16 +91,6 @@ __device__ __forceinline__ double inverse_root(double x) {
   s = s * __builtin_fma(-h * s, s, 1.5);
   return r > 0.0 && r < __builtin_inf() ? s : r;  // (x infinite, zero or NaN: r itself)
 }
-// y / scale as a division gives it, by scale's inverse: their product and one correction
-// (compared with the division over all of scale's fractions, at and beside the ties of
-// E4M3).  scale >= 2^-100, below which what is left over would pass fp32's range.
-template <bool FINITE>
-__device__ __forceinline__ float quotient(float y, float scale, float inverse) {
-  const float q = y * inverse;
-  const float r = copysignf(__builtin_fmaf(__builtin_fmaf(-q, scale, y), inverse, q), y);
-  return FINITE || fabsf(q) < 1e30f ? r : q;
-}
-
 // A token's row into the pool.  FINITE: no infinity and no NaN among its values.
 template <int FORMAT, bool FINITE>
 __device__ __forceinline__ void write_row(const MlaAppendLaunch& a, int32_t slot, int lane, float (&y)[8], float r, uint32_t top) {
