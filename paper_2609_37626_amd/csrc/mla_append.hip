@@ -11,11 +11,12 @@
 // it to their order.
 //
 // Bound: the instructions of a token, then HBM: 11.1k tokens into per-token E4M3 take
-// 8.2 us for 19 MB (2.8 us at the rate of reads).  From 11.0 us: sums and maxima over
-// lanes by row turns and lane reads rather than shuffles through LDS, 1 / sqrt by two
-// Newton steps, quotients by one inverse and a correction, finite values on a path of
-// their own (to 9.5), and every load of a token before the first wait (to 8.2).  A token
-// for each of 256 requests is launch latency: 3.4 us.
+// 8.5 us for 19 MB (2.8 us at the rate of reads), into bf16 or latent rows 7.9 and 8.0.
+// From 11.0 us: sums and maxima over lanes by row turns and lane reads rather than shuffles
+// through LDS, 1 / sqrt by two Newton steps, quotients by one inverse and a correction,
+// finite values on a path of their own (to 9.5), and every load of a token before the first
+// wait (to 8.2).  A token for each of 256 requests is launch latency: 3.4 us, 2.8 after
+// another kernel of a graph.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

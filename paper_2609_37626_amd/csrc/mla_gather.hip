@@ -6,7 +6,7 @@
 // all rows' loads in flight before the first store.
 //
 // Bound: HBM (1,152, 580 or 656 bytes read and 1,152 written a row): 67k rows of the
-// latent format are 122 MB in 19.5 us, 6.2 TB/s.  It is rows in flight that carry the
+// latent format are 122 MB in 20 us, 6.0 TB/s.  It is rows in flight that carry the
 // rate: bounds of six waves a SIMD took it from 32.6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -25,11 +25,12 @@
 //
 // Bound: matrix instructions, 320 multiplications and additions each a row and key of a
 // head (192 + 128), at 1.36 PFLOP/s of a large library product.  128 heads of one prompt
-// of 4096 rows: 697 us, 986 TFLOP/s; 32 of 2 x 4096 rows over 4096 more: 889 us, 1,160.
+// of 4096 rows: 705 us, 975 TFLOP/s; 32 of 2 x 4096 rows over 4096 more: 907 us, 1,136.
 // Of the first, the matrix instructions alone take 420 us, the loads into LDS 130, its
-// reads 100 and the softmax 80 that two waves a SIMD do not hide; a tile costs 8 us beside
-// its turns (loads of its first step and queries 3.4, writing the last one's rows 3.6, the
-// meeting of its waves 1.1), and a masked turn has 440 vector instructions, others 260.
+// reads 100 and the softmax 80 that two waves a SIMD do not hide (copies of the kernel
+// with the rest left out); a tile costs 8 us beside its turns (by the clock: loads of its
+// first step and queries 3.4, writing the last one's rows 3.6, the meeting of its waves
+// 1.1), and a masked turn has 440 vector instructions, others 260.
 //
 // W = 8: one workgroup fills a compute unit, four steps in LDS, two of them on the way;
 // W = 4: two do, two steps each.  The larger tile halves the loads a row and keeps long
@@ -66,9 +67,9 @@ constexpr float kLowest = -1e30f;             // the reference before any score
 // kLeast steps or more.  Places on the line count eighths of a step.  A piece costs 16 to
 // 18 us beside its steps of 2.1 (first loads, the diagonal, writing its part), kTileCost,
 // and a step of a tile of half the rows or less, a wave a SIMD instead of two, 0.65 of
-// others (95 us against 145).  Counted so, 8 heads of 8192 rows take 207 us, 20 of 382 and
-// 512 rows over 18k and 10k keys 192; with every step alike and a tile's cost of one 241
-// and 197.  (Costs of 4 and 12 steps: 211 and 214, 192 and 188.)
+// others (95 us against 145).  Counted so, 8 heads of 8192 rows take 186 us, 20 of 382 and
+// 512 rows over 18k and 10k keys 181; with every step alike and a tile's cost of one 234
+// and 194.  (Costs of 4 and 12 steps: 206 and 199, 185 and 187.)
 constexpr int32_t kNeverCut = 12;
 constexpr int32_t kLeast = 4;
 constexpr int32_t kStep = 8, kHalfStep = 5;
@@ -229,7 +230,7 @@ __device__ __forceinline__ Call look_at(const MlaPrefillLaunch& a) {
 // Block j counts as K - D j steps, K its request's last tile's: how many
 // blocks are longer than a length is a sum over the requests, and the rank's length
 // is found by halving.  Past 64 kSorted requests, and where all tiles begin at once anyway
-// (`sorted` false: 15.1 us for four short prompts, 15.6 sorted), the blocks go in the requests' order.
+// (`sorted` false: 15.2 us for four short prompts, 16.1 sorted), the blocks go in the requests' order.
 template <int ROWS>
 __device__ __forceinline__ bool find_block(const MlaPrefillLaunch& a, bool sorted, int32_t rank, int shift, Request& r, int32_t& block) {
   const int lane = threadIdx.x & 63;
@@ -1126,18 +1127,18 @@ hipError_t launch_tiles(const MlaPrefillLaunch& a, bool small, hipStream_t s) {
 
 hipError_t launch_mla_prefill(const MlaPrefillLaunch& a, hipStream_t s) {
   // From the call's averages: W = 8 where tiles will be cut or see 40 steps or more on
-  // average.  Measured (us, W = 4 / 8), cut: 8 heads of 16,384 rows 606 / 567, 20 of 2 x 512
-  // rows over 8192 keys 168 / 137, of 8 x 200 over 4000 174 / 143; long: 128 of 6144 rows
-  // 1,522 / 1,490, 32 of 8 x 1024 over 4096 784 / 721; else: 128 of 4096 rows 714 / 721, 32
-  // of 4 x 1024 83 / 96, 16 of 64 x 200 91 / 106.
+  // average.  Measured (us, W = 4 / 8), cut: 8 heads of 16,384 rows 623 / 562, 20 of 2 x 512
+  // rows over 8192 keys 161 / 141, of 8 x 200 over 4000 183 / 141; long: 128 of 6144 rows
+  // 1,496 / 1,463, 32 of 8 x 1024 over 4096 777 / 709; else: 128 of 4096 rows 701 / 699, 32
+  // of 4 x 1024 89 / 101, 16 of 64 x 200 95 / 108.
   const int64_t rows = max((int64_t)a.num_rows / a.B, (int64_t)1), keys = max((int64_t)a.num_keys / a.B, rows);
   const int64_t steps = (keys - rows / 2) / kKeys, tiles = (rows + 127) / 128 * a.B * a.heads;
   const bool cut = keys > kNeverCut * kKeys && keys / kKeys * 2 * a.units > tiles * steps;
   if (cut || steps >= 40) return launch_tiles<8>(a, false, s);
   // A workgroup each for a few short tiles: they are over before the order's launch is made
-  // up for (us, a workgroup each / one after the other: 32 heads of 34 x 18 rows 26.8 / 30.3,
-  // 16 of 64 x 250 96 / 103, 8 of 100 x 60 32 / 36; but 128 of 64 x 8 130 / 123, 64 of
-  // 10 x 500 151 / 143).
+  // up for (us, a workgroup each / one after the other: 32 heads of 34 x 18 rows 28 / 32, 8 of
+  // 100 x 60 34 / 38; but with more than four for each that stays 128 of 64 x 8 132 / 130, 64
+  // of 10 x 500 153 / 150, 16 of 64 x 250 108 / 110).
   return launch_tiles<4>(a, keys < 384, s);
 }
 

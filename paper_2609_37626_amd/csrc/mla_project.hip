@@ -135,7 +135,7 @@ __global__ __launch_bounds__(kThreads, 2) void mla_absorb_kernel(MlaAbsorbLaunch
   }
   const uint32_t chunks = ((uint32_t)a.num_tokens + chunk - 1) / chunk;
   // A head's four blocks on one XCD, which then reads its queries once (256 tokens of 128
-  // heads: 15.0 us, 16.4 with the blocks apart), where the heads fill the XCDs evenly.
+  // heads: 15.6 us, 17.0 with the blocks apart), where the heads fill the XCDs evenly.
   constexpr uint32_t kColumnBlocks = kDimV / kColumns;
   const bool even = a.heads % 8 == 0;
   uint32_t item, part;
@@ -303,7 +303,7 @@ hipError_t launch_expand(const MlaExpandLaunch& a, hipStream_t s) {
 
 hipError_t launch_mla_expand(const MlaExpandLaunch& a, hipStream_t s) {
   // The fewest tokens a workgroup (32, 64 or 128) with which all of them begin at once, one
-  // a compute unit: 635 tokens of 8 heads take 7.5 us so, 11.1 at 128.
+  // a compute unit: 635 tokens of 8 heads take 5.6 us so, 10.8 at 128.
   const auto groups = [&](int64_t tokens) { return a.heads * ((a.num_tokens + tokens - 1) / tokens); };
   if (groups(32) <= 256) return launch_expand<1>(a, s);
   return groups(64) <= 256 ? launch_expand<2>(a, s) : launch_expand<4>(a, s);
