@@ -702,15 +702,15 @@ int splash_mla_expand_out(const void* out, const void* w_uv, int64_t w_head_stri
  *         what one call leaves for its own second launch, and calls that may overlap
  *         take one each
  * Products are summed in fp32; a weight is rounded to bf16 where it meets V (2^-8), its
- * sum is not.  Weights are taken against an earlier score than the row's largest, up to
- * 128 a key on average: finite values past 2^120 / nk may overflow the sum to an
- * infinity or NaN.  Keys that a row does not see do not touch it, whatever they hold
- * (NaN and infinities in k, key and v among them); a score that is NaN or +inf makes its
- * row NaN.  An infinity or NaN in a v that a row sees makes that value of the row
- * infinite (both signs: NaN) or NaN, whatever the key's weight, unless the row has no
- * weight at all (every score -inf: out = 0, lse = -inf).  A score's own rounding, 2^-24
- * of it, is its weight's relative error: rows whose scores pass 2^20 mean little, and
- * past 2^30 may be NaN.  Deterministic: the same inputs and sizes give the same bits.
+ * sum is not.  Weights in the sum are 1/8 a key at most on average: finite values past
+ * 2^129 / nk may overflow it to an infinity or NaN.  Keys that a row does not see do not
+ * touch it, whatever they hold (NaN and infinities in k, key and v among them); a score
+ * that is NaN or +inf makes its row NaN.  An infinity or NaN in a v that a row sees
+ * makes that value of the row infinite (both signs: NaN) or NaN, whatever the key's
+ * weight, unless the row has no weight at all (every score -inf: out = 0, lse = -inf).
+ * A score's own rounding, 2^-24 of it, is its weight's relative error: rows whose scores
+ * pass 2^20 mean little, and past 2^30 may be NaN.  Deterministic: the same inputs and
+ * sizes give the same bits.
  * Errors: INVALID_ARGUMENT (NULL, negative counts or strides, softmax_scale not
  * finite and > 0), UNSUPPORTED (num_heads past 1024, num_rows or num_keys past 2^25,
  * batch past 2^20, a token stride past 2^24, num_rows * num_heads past 2^31 - 1,

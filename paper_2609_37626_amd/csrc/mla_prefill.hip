@@ -15,11 +15,11 @@
 // dealt out between the matrix instructions, then PV of the last turn: a step's values
 // are the second half of the step before and the first of its own.
 //
-// The softmax runs over the keys once with a reference that moves only where a lane's
-// eight weights of a row pass 1024: below that no sum of weights can overflow, and the lane
-// needs no maximum and no exchange for it, only the sum that it makes anyway.  A row's nk
-// weights are 128 nk at most together (32 of the first turn, 4096 of each other one), so
-// that values up to 2^120 / nk stay in fp32's range.  Each row decides by its own scores:
+// The softmax runs over the keys once with a reference 2^10 above the largest score, which
+// moves only where a lane's eight weights of a row pass 1: below that no sum of weights can
+// overflow, and the lane needs no maximum and no exchange for it, only the sum that it makes
+// anyway.  A row's nk weights are nk / 8 at most together (2^-5 of the first turn, 4 of each
+// other one), so that values up to 2^129 / nk stay in fp32's range.  Each row decides by its own scores:
 // other rows' values do not reach its result (their lengths do, where tiles are cut: the
 // cuts' places are the whole call's, and the order of a row's sums with them).
 //
@@ -60,7 +60,8 @@ constexpr int kKeyBytes = 3 * kGroupBytes;    // a step's keys in LDS
 constexpr int kStepBytes = 5 * kGroupBytes;   // and its values after them
 constexpr int kLoads = 40;                    // loads to LDS a step, by all waves
 constexpr int kAhead = 4;                     // operands read ahead
-constexpr float kMost = 1024.f;               // a lane's eight weights of a row, before the reference moves
+constexpr float kMost = 1.f;                  // a lane's eight weights of a row, before the reference moves
+constexpr float kAbove = 10.f;                // powers of two from a row's largest score up to where it moves
 constexpr float kLowest = -1e30f;             // the reference before any score
 // A cut tile's parts pass through memory and a second launch joins them (6 us): tiles of
 // at most kNeverCut steps, 768 keys, do not wait as long, and a worker of the line gets
@@ -343,6 +344,12 @@ __device__ __forceinline__ float row_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
+// A row's LSE from its reference and sum (both brought back by kAbove first: a logarithm near
+// -10 would be off by more).
+__device__ __forceinline__ float natural_lse(float top, float l) {
+  return l == 0.f ? -INFINITY : (top - kAbove + __log2f(l * 1024.f)) * 0.69314718055994530942f;
+}
+
 // Softmax and products of a tile's steps [step0, step1) in this workgroup's waves;
 // `before` runs once the first loads are on their way (p still holds the last tile),
 // `after` once the wave has multiplied all that it sees, while others still do.
@@ -502,7 +509,7 @@ __device__ __forceinline__ void attend(const MlaPrefillLaunch& a, const Tile& ti
     for (int r = 0; r < R; ++r) {
       float most = fmaxf(s[r], __shfl_xor(s[r], 16));
       most = fmaxf(most, __shfl_xor(most, 32));
-      const float m = highest(z, r), to = most > kMost ? m : top[r], by = __builtin_amdgcn_exp2f(top[r] - to);
+      const float m = highest(z, r), to = most > kMost ? m + kAbove : top[r], by = __builtin_amdgcn_exp2f(top[r] - to);
       top[r] = to;
       sum[r] *= by;
 #pragma unroll
@@ -734,7 +741,7 @@ __device__ __forceinline__ void write_rows(const MlaPrefillLaunch& a, const Tile
       const auto hi = __builtin_amdgcn_permlane16_swap(v[0][1], v[1][1], false, false);
       *(u32x4*)(to + 16 * d) = (u32x4){lo[0], hi[0], lo[1], hi[1]};
     }
-    if (a.lse && g == 0) a.lse[n] = l == 0.f ? -INFINITY : (p.top[r] + __log2f(l)) * 0.69314718055994530942f;
+    if (a.lse && g == 0) a.lse[n] = natural_lse(p.top[r], l);
   }
 }
 template <int W>
@@ -1093,7 +1100,7 @@ __global__ __launch_bounds__(kThreads) void mla_prefill_join_kernel(MlaPrefillLa
   hi *= by;
   *(u32x4*)(a.out + n * kValue + 8 * lane) =
       (u32x4){pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]), pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3])};
-  if (a.lse && lane == 0) a.lse[n] = sum == 0.f ? -INFINITY : (top + __log2f(sum)) * 0.69314718055994530942f;
+  if (a.lse && lane == 0) a.lse[n] = natural_lse(top, sum);
 }
 
 template <int W>

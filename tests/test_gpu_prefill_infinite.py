@@ -191,17 +191,17 @@ def test_rows_that_see_no_key_in_long_calls(new, old, heads):
             assert bool(((lse[n].double().cpu() - torch.logsumexp(z, 0)).abs() <= 198 * 2.0 ** -18 + 2.0 ** -10).all())
 
 
-@pytest.mark.parametrize("new,old,heads", [([200], [824], 2), ([40], [6000], 1), ([1024], [4096], 72)])
+@pytest.mark.parametrize("new,old,heads", [([200], [824], 2), ([40], [6000], 1), ([1024], [4096], 72), ([3], [0], 1)])
 def test_values_at_the_end_of_the_range(new, old, heads):
-    """Values of 2^120 / nk and weights that come close to 128 each: all scores behind the first 32 keys 6.8 powers of two
-    above theirs, which moves no reference."""
+    """Values of 2^129 / nk or the type's largest power of two, and weights that come close to the most that moves no
+    reference: all scores behind the first 32 keys 6.8 powers of two above theirs."""
     p = Prompts(new, old, heads, seed=6)
     keys, ones = int(p.keys[0]), np.uint16(0x3F80)
     p.q[:], p.kv[..., :128], p.key[:] = 0, 0, 0
     p.q[..., 0] = ones
     p.scale = np.float32(6.8 * np.log(2.0))
     p.kv[32:, :, 0] = ones
-    p.kv[..., 128:] = (p.kv[..., 128:] & 0x8000) + ((127 + 120 - int(np.ceil(np.log2(keys)))) << 7)
+    p.kv[..., 128:] = (p.kv[..., 128:] & 0x8000) + ((127 + min(127, 129 - int(np.ceil(np.log2(keys))))) << 7)
     p.kv[..., 128:160] &= 0x7FFF      # sums of one sign
     out, lse = p.run()
     some = sorted({0, heads - 1})
